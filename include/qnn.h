@@ -78,7 +78,16 @@ typedef enum QNN_ENUM_INT {
     QNN_ERR_ALLOC = 8        /* device or host allocation failed */
 } qnn_status;
 
-typedef enum QNN_ENUM_INT { QNN_UINT8 = 0, QNN_INT8 = 1, QNN_INT32 = 2 } qnn_dtype;
+/* QNN_FLOAT16 and QNN_BFLOAT16 are taken by the 4-bit cache and its attention
+ * only; their values are the real ones, so that qparams beside them are not
+ * read. */
+typedef enum QNN_ENUM_INT {
+    QNN_UINT8 = 0,
+    QNN_INT8 = 1,
+    QNN_INT32 = 2,
+    QNN_FLOAT16 = 3,
+    QNN_BFLOAT16 = 4
+} qnn_dtype;
 
 /* Rounding of the fixed-point requantize (the paper leaves it to the
  * framework, Sec. III-B): HALF_UP rounds round(v * mult / 2^shift) with ties
@@ -259,6 +268,144 @@ qnn_status qnn_pool2d(void *stream, const void *x, qnn_dtype dtype, int32_t N, i
                       int32_t W, int32_t C, int32_t R, int32_t S, qnn_conv_params pool,
                       qnn_pool_mode mode, int32_t count_pad, int32_t zero_point, void *y,
                       qnn_rounding rounding);
+
+/* ---------------------------------------------------------------- 4-bit cache */
+
+/*
+ * Keys and values of a transformer's attention, held as quantized tensors of
+ * Eq. (1) with 4-bit codes: each vector (one token, one head, K or V) has its
+ * own scale s and zero point z, and stands for s * (c - z), c and z in 0..15.
+ * The cache is device memory of the caller: `pages` pages of page_size tokens
+ * for `heads` heads of head_dim values. A token's slot is page * page_size +
+ * its place in the page.
+ *   page_size: 16, 32, 64, 128 or 256; head_dim: a multiple of 8, 8 to 256;
+ *   data: 16-byte aligned, pages * qnn_cache4_page_bytes() bytes; pages *
+ *   page_size below 2^31.
+ * Layout, with DP = head_dim rounded up to 64, 128 or 256: a page is a block
+ * of page_size * (DP + 8) bytes for each head:
+ *   K codes   token t's row of DP / 2 bytes at t * DP / 2; of each 4-byte word
+ *             (channels 8w .. 8w + 7) bits 4i .. 4i + 3 hold channel 8w + 2i
+ *             (i < 4) or 8w + 2(i - 4) + 1;
+ *   V codes   tiles of eight tokens, [16][DP / 64][8 tokens] of 2 bytes: unit
+ *             (u, j) of a token holds channels u * DP / 16 + 4j + 0 .. 3, the
+ *             first in the low bits;
+ *   records   page_size 32-bit words for K, then as many for V: the f32 bits of
+ *             s, of which the low 8 are 0, or'ed with z.
+ * Channels past head_dim hold anything.
+ */
+typedef struct {
+    void *data;
+    int32_t pages, page_size, heads, head_dim;
+} qnn_cache4;
+
+/* Bytes of one page, 0 for sizes that the cache does not take. */
+size_t qnn_cache4_page_bytes(int32_t page_size, int32_t heads, int32_t head_dim);
+
+/*
+ * Quantizes K and V of `tokens` tokens to 4 bits and stores token i at
+ * slots[i] (device int32). A slot below 0 or past the last page is skipped:
+ * its rows are not even read. Slots of one call differ from each other.
+ *   k, v: device, dtype UINT8 / INT8 (values s * (q - zp) of k_q, v_q, per
+ *      tensor) or FLOAT16 / BFLOAT16; element (i, h, d) at i * ld + h *
+ *      head_dim + d, ld >= heads * head_dim; rows aligned to 8 elements
+ *      (QNN_ERR_UNSUPPORTED else).
+ * With lo = min(0, min x) and hi = max(0, max x) of a vector's values in f32:
+ * s = (hi - lo) / 15, rounded up to a 16-bit significand, z = round(-lo / s),
+ * c = clamp(round(x / s) + z, 0, 15), ties to even; a vector of zeros has
+ * s = 0. NaN counts as 0, and values beyond +-2^126 as that.
+ * Enqueued on `stream`, no synchronization.
+ */
+qnn_status qnn_cache4_append(void *stream, qnn_cache4 cache, const void *k, const void *v, qnn_dtype dtype,
+                             qnn_qparams k_q, qnn_qparams v_q, int32_t tokens, int64_t k_ld, int64_t v_ld,
+                             const int32_t *slots);
+
+/*
+ * Reads the vectors at slots[i] back as s * (c - z), rounded to dtype
+ * (FLOAT16 or BFLOAT16): element (i, h, d) at i * ld + h * head_dim + d. Slots
+ * below 0 or past the last page give zeros. k or v may be NULL: not read.
+ * Enqueued on `stream`, no synchronization.
+ */
+qnn_status qnn_cache4_read(void *stream, qnn_cache4 cache, const int32_t *slots, int32_t tokens, void *k, void *v,
+                           qnn_dtype dtype, int64_t k_ld, int64_t v_ld);
+
+/*
+ * Attention of queries over the 4-bit cache:
+ *   o = sum_t p_t V_t / sum_t p_t,  p_t = exp(scale * q . K_t),
+ * over the tokens t that a query sees. Both products are Eq. (3): the codes
+ * are multiplied as they are and the zero points' terms taken off,
+ *   q . K_t = s_t * (sum_d q_d c_td - z_t sum_d q_d).
+ * Request b has ctx[b] tokens in the cache, token t in page table[b * table_ld
+ * + t / page_size], and queries cu_q[b] .. cu_q[b + 1] - 1 (cu_q NULL: one
+ * query each, `tokens` == requests). Its last query is at position ctx[b] - 1,
+ * and a query at position p sees tokens t < ctx[b], with causal != 0 those
+ * t <= p, with window > 0 those t > p - window. A query that sees none (ctx[b]
+ * of 0, or fewer tokens than queries) gives 0. Tokens past table_width pages
+ * or in a page outside [0, pages) are not seen; such entries are not read
+ * through.
+ *   q: device [tokens][q_heads][head_dim], row stride q_ld, UINT8 / INT8 (q_q
+ *      per tensor) or FLOAT16 / BFLOAT16; query head h reads the cache's head
+ *      h / (q_heads / heads), q_heads a multiple of heads.
+ *   max_q: at least the queries of any one request, and max_ctx (0: as many as
+ *      the table holds) about the tokens of the longest: they shape the grid.
+ *      Queries past max_q are not computed; max_ctx affects the speed only.
+ *   o: device [tokens][q_heads][head_dim], row stride o_ld, FLOAT16, BFLOAT16,
+ *      or UINT8 / INT8 (o_q per tensor): round(o / s) + zp, ties to even,
+ *      clamped to the dtype. Rows of no request (cu_q[requests] on) are left
+ *      as they were. Must not overlap q.
+ *   workspace: device, 16-byte aligned, of at least
+ *      qnn_attention4_workspace_size() bytes (NULL if that is 0), read and
+ *      written by this call alone until it is done; contents do not matter.
+ * Rows of q and o are aligned to 8 elements (QNN_ERR_UNSUPPORTED else).
+ * Scores, the softmax and sums are f32; q enters the matrix cores as f16
+ * scaled by a power of two (exact for f16, and 8-bit values), each weight
+ * p_t s_t as f16. Enqueued on `stream`, no synchronization.
+ */
+typedef struct {
+    int32_t tokens, q_heads, requests, table_width;
+    int64_t q_ld, o_ld, table_ld;
+    int32_t max_q, max_ctx, causal, window;
+    float scale;
+} qnn_attention_params;
+
+size_t qnn_attention4_workspace_size(qnn_cache4 cache, qnn_attention_params p);
+
+qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qparams q_q, qnn_cache4 cache,
+                          const int32_t *table, const int32_t *ctx, const int32_t *cu_q, qnn_attention_params p,
+                          void *o, qnn_dtype o_dtype, qnn_qparams o_q, void *workspace, size_t workspace_bytes);
+
+/*
+ * Brings the block tables of `requests` requests from lens[b] to new_lens[b]
+ * tokens (all arrays on the device): requests that shrink give the pages past
+ * ceil(new / page_size) back, requests that grow take new ones, and every new
+ * token gets its slot.
+ *   table: row b (stride table_ld, table_width entries) lists b's pages; given
+ *      up entries become -1, entries past the old length are not read.
+ *   free_pages: a stack of free_capacity entries, *free_count of them in use,
+ *      the last on top. Pages are given back and taken in order of request,
+ *      then of place: the i-th given back goes to entry n - 1 - i, n the count
+ *      after all of them, and the i-th taken comes from entry m - 1 - i, m the
+ *      count before, with those just given back. So giving back what one call
+ *      took restores the stack.
+ *   lens, *free_count: updated.
+ *   cu: [requests + 1], the new tokens' running count.
+ *   slots, positions: [token_capacity]; request b's new tokens at cu[b] on, in
+ *      order: slot, and position in the request (lens[b] on). Entries past the
+ *      last are -1 and 0. positions may be NULL.
+ *   status: 0: done. Else nothing is changed, cu is 0 and slots are -1:
+ *      n > 0: n pages are missing; -1: a length below 0 or beyond the table,
+ *      or *free_count outside [0, free_capacity]; -2: more new tokens than
+ *      token_capacity; -3: more given back than the stack holds.
+ *   workspace: device, 16-byte aligned, qnn_pages_workspace_size(requests)
+ *      bytes, used by this call alone until it is done.
+ * page_size: a power of two, 1 to 4096. Enqueued on `stream`, no
+ * synchronization.
+ */
+size_t qnn_pages_workspace_size(int32_t requests);
+
+qnn_status qnn_pages_resize(void *stream, int32_t requests, int32_t page_size, int32_t *lens, const int32_t *new_lens,
+                            int32_t *table, int32_t table_width, int64_t table_ld, int32_t *free_pages,
+                            int32_t free_capacity, int32_t *free_count, int32_t *cu, int32_t *slots,
+                            int32_t *positions, int32_t token_capacity, int32_t *status, void *workspace);
 
 /* ---------------------------------------------------------------- plans */
 

@@ -1,0 +1,584 @@
+// Attention over the 4-bit cache (qnn_attention4; the cache's layout is in
+// include/qnn.h).
+//
+// Mathematics.  K_t = s_t (c_t - z_t) and V_t = s'_t (c'_t - z'_t), so with
+// y_t = scale log2(e) q . K_t
+//   q . K_t = s_t (sum_d q_d c_td - z_t sum_d q_d)
+//   o_d = (sum_t w_t c'_td - sum_t w_t z'_t) / sum_t p_t,
+//         p_t = 2^(y_t - u), w_t = p_t s'_t
+// for any u (the terms of Eq. (3): codes multiplied as they are, the zero
+// points' parts taken off). Both products run on the f16 matrix cores, which
+// take the codes without any conversion: a code c in bits 0 .. 3 of an f16 is
+// the subnormal c * 2^-24, and at bits 4 .. 7 it is c * 2^-20. Eight codes cost
+// seven instructions. The cores cut each product some 27 bits below the
+// largest that its operands' exponent fields allow (measured: sums of 32 codes
+// by weights up to 1 are off by up to 2^-12 with codes at bit 0, 2^-16.2 at bit
+// 4, 2^-16.6 with codes as ordinary f16 numbers), so bits 4 .. 7 it is: as
+// exact as f32 sums.
+//
+// A wave holds 16 R query rows (a request's queries times the heads that share
+// a cache head) and walks the tokens 32 at a time:
+//   scores^T [token][row] = K q^T: a lane then has eight neighbouring tokens of
+//   one row, which is exactly the operand that
+//   o^T [channel][row] += V^T p^T wants: the weights never leave the lane.
+// The running offset u of a row is raised only when a weight would leave
+// f16's or a sum f32's comfortable range (w > 2^8 or sum p > 2^98); the
+// output is linear in the weights, so any u gives the same quotient.
+//
+// The four waves of a workgroup take every fourth 32 tokens and are joined
+// through LDS.
+#include "cache4.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace qnn {
+namespace {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+struct AttnArgs {
+    Cache4Args c;
+    const void *q;
+    void *o;
+    const int32_t *table, *ctx, *cu;
+    int64_t q_ld, o_ld, table_ld;
+    int32_t q_dt, o_dt;
+    int32_t tokens, requests, q_heads, group;   // group: query heads of a cache head
+    int32_t width, max_q, causal, window;
+    int32_t tiles;          // row tiles of a request and cache head
+    int32_t total;          // workgroups with work, at most
+    float scale;            // scale * log2(e), times the query's own scale
+    int32_t q_zp;
+    float o_scale;
+    int32_t o_zp, o_lo, o_hi;
+};
+
+constexpr int kWaves = 4;
+constexpr uint32_t kCode = 0x00f000f0u;   // a code at bits 4 .. 7 of each half: c * 2^-20
+constexpr float kNone = -1e30f;      // offset of a row without tokens yet
+constexpr float kMaxWeight = 256.0f, kMaxSum = 0x1p98f;
+
+// Tokens [lo, hi) that rows first .. last - 1 of a request see between them; a
+// row is a query (row / group) and one of the heads.
+struct Span {
+    int lo, hi;
+};
+__device__ __forceinline__ Span seen(const AttnArgs &a, int ctx, int nq, int query_first, int query_last)
+{
+    const int held = min(ctx, a.width << a.c.shift);
+    const int p0 = ctx - nq + query_first, p1 = ctx - nq + query_last;   // positions
+    Span s;
+    s.hi = a.causal ? min(held, p1 + 1) : held;
+    s.lo = a.window > 0 && p0 >= a.window ? p0 - a.window + 1 : 0;
+    return s;
+}
+
+// max over the four lanes that hold a row's tokens
+__device__ __forceinline__ float row_max(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// Eight query values of element type dt at p.
+__device__ __forceinline__ void load_q8(const uint8_t *p, int dt, int zp, float (&x)[8])
+{
+    if (dt == QNN_FLOAT16) {
+        const h8 h = *(const h8 *)p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i] = (float)h[i];
+    } else if (dt == QNN_BFLOAT16) {
+        const u4 w = *(const u4 *)p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i] = __builtin_bit_cast(float, i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    } else {
+        const u2 w = *(const u2 *)p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t b = (w[i >> 2] >> (8 * (i & 3))) & 0xffu;
+            x[i] = (float)((dt == QNN_INT8 ? (int)(int8_t)b : (int)b) - zp);
+        }
+    }
+}
+
+// Stores N = 4, 8 or 16 neighbouring output values at element offset `at`.
+template <int N>
+__device__ __forceinline__ void store_out(const AttnArgs &a, int64_t at, const float (&v)[N])
+{
+    if (a.o_dt == QNN_FLOAT16 || a.o_dt == QNN_BFLOAT16) {
+        uint32_t w[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            if (a.o_dt == QNN_FLOAT16)
+                w[i] = __builtin_bit_cast(uint32_t, h2{(_Float16)v[2 * i], (_Float16)v[2 * i + 1]});
+            else
+                w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i]) |
+                       (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i + 1]) << 16;
+        }
+        uint32_t *p = (uint32_t *)((uint8_t *)a.o + at * 2);
+#pragma unroll
+        for (int i = 0; i < N / 2; i += 2)
+            *(u2 *)(p + i) = u2{w[i], w[i + 1]};
+    } else {
+        uint32_t w[N / 4];
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            w[i] = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // beyond the clamp before the integer conversion; NaN gives the zero point
+                const float t = fminf(fmaxf(__builtin_rintf(v[4 * i + e] / a.o_scale), -1024.0f), 1024.0f);
+                const int code = v[4 * i + e] == v[4 * i + e] ? (int)t + a.o_zp : a.o_zp;
+                w[i] |= ((uint32_t)min(max(code, a.o_lo), a.o_hi) & 0xffu) << (8 * e);
+            }
+        }
+        uint32_t *p = (uint32_t *)((uint8_t *)a.o + at);
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i)
+            p[i] = w[i];
+    }
+}
+
+template <int DP, int R>
+__global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
+{
+    constexpr int KS = DP / 32;    // K-steps of a score; words of K of a lane and token
+    constexpr int NV = DP / 16;    // 16-channel blocks of the output
+    constexpr int NW = DP / 64;    // 16-byte pieces of V of a lane (eight tokens, four channels each)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, g = lane >> 4;
+
+    // XCD x takes the x-th eighth of the list: the row tiles of one cache head
+    // follow each other there, the longest (causal) first
+    const int share = (a.total + 7) >> 3;
+    const int xcd = blockIdx.x & 7;
+    int work = xcd * share + (blockIdx.x >> 3);
+    if (work >= min(a.total, (xcd + 1) * share))
+        return;
+    const int tile = a.tiles - 1 - work % a.tiles;
+    work /= a.tiles;
+    const int kvh = work % a.c.heads, b = work / a.c.heads;
+    const int first = a.cu ? min(max(a.cu[b], 0), a.tokens) : b;
+    const int nq = a.cu ? min(max(min(a.cu[b + 1], a.tokens) - first, 0), a.max_q) : 1;
+    const int rows = nq * a.group, row0 = tile * 16 * R;
+    if (row0 >= rows)
+        return;
+    const int ctx = max(a.ctx[b], 0);
+    const Span span = seen(a, ctx, nq, row0 / a.group, (min(row0 + 16 * R, rows) - 1) / a.group);
+
+    // ---- queries, as the second operand: lane (n, g) holds channels 8 (g KS +
+    // k) .. + 7 of row n for step k
+    u4 q[R][KS];
+    float qsum[R], fac[R];
+    int lo_row[R], hi_row[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = row0 + r * 16 + n;
+        const bool live = row < rows;
+        const int i = live ? row / a.group : 0, h = live ? row - i * a.group : 0;
+        const Span own = seen(a, ctx, nq, i, i);
+        lo_row[r] = own.lo;
+        hi_row[r] = own.hi;
+        float x[KS][8], most = 0.0f;
+        const int esize = a.q_dt == QNN_FLOAT16 || a.q_dt == QNN_BFLOAT16 ? 2 : 1;
+        const uint8_t *p = (const uint8_t *)a.q +
+                           ((int64_t)(first + i) * a.q_ld + (int64_t)(kvh * a.group + h) * a.c.dim) * esize;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int ch = 8 * (g * KS + k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x[k][e] = 0.0f;
+            if (live && ch < a.c.dim)
+                load_q8(p + ch * esize, a.q_dt, a.q_zp, x[k]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                most = fmaxf(most, fabsf(x[k][e]));
+        }
+        most = row_max(most);
+        // a power of two brings the row's largest to 2^14 .. 2^15: exact for 8-bit
+        // and f16 values, and values of any exponent fit f16
+        const int ex = (int)(__builtin_bit_cast(uint32_t, most) >> 23);   // 255: not finite, stays as it is
+        const float up = ex == 255 ? 1.0f : __builtin_bit_cast(float, (uint32_t)min(127 + 14 + 127 - ex, 253) << 23);
+        const float sgn = a.scale < 0.0f ? -up : up;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            h8 h8v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h8v[e] = (_Float16)(x[k][e] * sgn);
+                sum += (float)h8v[e];
+            }
+            q[r][k] = __builtin_bit_cast(u4, h8v);
+        }
+        qsum[r] = row_sum(sum) * 0x1p-20f;
+        // least above 0, so that a masked score (-inf) stays one
+        fac[r] = fmaxf(fabsf(a.scale) * 0x1p20f / up, 0x1p-126f);
+    }
+
+    f4 acc[R][NV], zacc[R];
+    float off[R], total[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            acc[r][j] = f4{0, 0, 0, 0};
+        zacc[r] = f4{0, 0, 0, 0};
+        off[r] = kNone;
+        total[r] = 0.0f;
+    }
+
+    const int P = 1 << a.c.shift;
+    const int32_t *const table = a.table + b * a.table_ld;
+    const uint8_t *const data = a.c.data + (size_t)kvh * a.c.head_bytes;
+    // page of token t (a token past the last looks up the last), -1 if the table's entry is none
+    auto page_of = [&](int t) {
+        const int p = table[min(t, span.hi - 1) >> a.c.shift];
+        return (unsigned)p < (unsigned)a.c.pages ? p : -1;
+    };
+    for (int t0 = (span.lo & ~31) + wave * 32; t0 < span.hi; t0 += kWaves * 32) {
+        // lane (n, g): K of tokens 8 (n / 4) + n % 4 (+ 4), words g KS on; V and
+        // records of tokens 8 g .. + 7, V's unit n
+        const int tk = t0 + (n >> 2) * 8, tv = t0 + g * 8;
+        const int pk = page_of(tk), pv = page_of(tv);
+        const uint8_t *const bk = data + (size_t)max(pk, 0) * a.c.page_bytes;
+        const uint8_t *const bv = data + (size_t)max(pv, 0) * a.c.page_bytes;
+        uint32_t kw[2][KS];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint32_t *p =
+                (const uint32_t *)(bk + ((tk & (P - 1)) + s * 4 + (n & 3)) * (DP / 2)) + g * KS;
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                kw[s][k] = p[k];
+        }
+        u4 vw[NW];
+        const u4 *const vp = (const u4 *)(bv + P * (DP / 2) + ((tv & (P - 1)) >> 3) * (4 * DP)) + n * NW;
+#pragma unroll
+        for (int j = 0; j < NW; ++j)
+            vw[j] = vp[j];
+        uint32_t rk[8], rv[8];
+        const uint32_t *const rp = (const uint32_t *)(bv + P * DP) + (tv & (P - 1));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            rk[j] = rp[j];
+            rv[j] = rp[P + j];
+        }
+
+        // ---- scores: sc[r][j] of token tv + j
+        f4 sc[R][2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                sc[r][s] = f4{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const uint32_t w = kw[s][k];
+                const u4 c = u4{w << 4 & kCode, w & kCode, w >> 4 & kCode, w >> 8 & kCode};
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    sc[r][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                        __builtin_bit_cast(h8, c), __builtin_bit_cast(h8, q[r][k]), sc[r][s], 0, 0, 0);
+            }
+        }
+        float vs[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            // a token that no row sees, or of no page, may hold anything
+            const bool held = tv + j >= span.lo && tv + j < span.hi && pv >= 0;
+            vs[j] = held ? rec_scale(rv[j]) : 0.0f;
+            const float ks = rec_scale(rk[j]), kz = rec_zero(rk[j]);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float x = __builtin_fmaf(-kz, qsum[r], sc[r][j >> 2][j & 3]) * (ks * fac[r]);
+                const bool sees = held && tv + j >= lo_row[r] && tv + j < hi_row[r];
+                sc[r][j >> 2][j & 3] = sees ? x : -INFINITY;
+            }
+        }
+        u4 pw[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float p[8], w[8], sum, top;
+            auto weigh = [&]() {
+                sum = 0.0f;
+                top = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    p[j] = __builtin_amdgcn_exp2f(sc[r][j >> 2][j & 3] - off[r]);
+                    w[j] = p[j] * vs[j];
+                    sum += p[j];
+                    top = fmaxf(top, w[j]);
+                }
+            };
+            weigh();
+            if (__any(top > kMaxWeight || sum > kMaxSum)) {
+                // raise the offset: the largest weight becomes 1 (or, where V's scales
+                // are below 2^-90, the largest p 2^90)
+                float most = kNone;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = sc[r][j >> 2][j & 3];
+                    most = fmaxf(most, fmaxf(x + __builtin_amdgcn_logf(vs[j]), x - 90.0f));
+                }
+                most = fmaxf(row_max(most), off[r]);
+                const float down = __builtin_amdgcn_exp2f(off[r] - most);
+                off[r] = most;
+                total[r] *= down;
+                zacc[r] *= down;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    acc[r][j] *= down;
+                weigh();
+            }
+            total[r] += sum;
+            h8 h;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                h[j] = (_Float16)w[j];   // rounded to nearest: 2^-12 of each weight at most, in no direction
+            pw[r] = __builtin_bit_cast(u4, h);
+        }
+        // ---- output: V's pieces hold pairs of tokens of four channels
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                u4 c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    c[e] = (i == 0 ? vw[v][e] << 4 : vw[v][e] >> (4 * i - 4)) & kCode;
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    acc[r][v * 4 + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                        __builtin_bit_cast(h8, c), __builtin_bit_cast(h8, pw[r]), acc[r][v * 4 + i], 0, 0, 0);
+            }
+        }
+        // sum w z by the same cores, every row of the operand z
+        u4 z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            z[e] = __builtin_amdgcn_perm(rv[2 * e + 1], rv[2 * e], 0x0c040c00u) << 4;   // low bytes
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            zacc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, z), __builtin_bit_cast(h8, pw[r]),
+                                                             zacc[r], 0, 0, 0);
+    }
+
+    // ---- the waves' parts joined: common offset, sums through LDS
+    __shared__ float offs[kWaves][R * 16];
+    __shared__ float sums[2][R * (NV * 4 + 1)][64];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        total[r] = row_sum(total[r]);
+        if (g == 0)
+            offs[wave][r * 16 + n] = off[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float most = kNone;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            most = fmaxf(most, offs[w][r * 16 + n]);
+        const float down = __builtin_amdgcn_exp2f(off[r] - most);
+        off[r] = most;
+        total[r] *= down;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            acc[r][j] = (acc[r][j] - zacc[r]) * (down * 0x1p20f);
+    }
+    auto put = [&](int slot) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    sums[slot][r * (NV * 4 + 1) + j * 4 + e][lane] = acc[r][j][e];
+            sums[slot][r * (NV * 4 + 1) + NV * 4][lane] = total[r];
+        }
+    };
+    auto take = [&](int slot) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[r][j][e] += sums[slot][r * (NV * 4 + 1) + j * 4 + e][lane];
+            total[r] += sums[slot][r * (NV * 4 + 1) + NV * 4][lane];
+        }
+    };
+    if (wave >= 2)
+        put(wave - 2);
+    __syncthreads();
+    if (wave < 2)
+        take(wave);
+    __syncthreads();
+    if (wave == 1)
+        put(0);
+    __syncthreads();
+    if (wave != 0)
+        return;
+    take(0);
+
+    // ---- lane (n, g) has channels (4 g + e) NV + j of row n
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = row0 + r * 16 + n;
+        if (row >= rows)
+            continue;
+        const int i = row / a.group, h = row - i * a.group;
+        const int64_t at = (int64_t)(first + i) * a.o_ld + (int64_t)(kvh * a.group + h) * a.c.dim;
+        const float inv = total[r] == 0.0f ? 0.0f : 1.0f / total[r];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int ch = (g * 4 + e) * NV;
+            if constexpr (NV == 16) {
+                float v[8];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        v[j] = acc[r][half * 8 + j][e] * inv;
+                    if (ch + half * 8 < a.c.dim)
+                        store_out(a, at + ch + half * 8, v);
+                }
+            } else {
+                float v[NV];
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    v[j] = acc[r][j][e] * inv;
+                if (ch < a.c.dim)
+                    store_out(a, at + ch, v);
+            }
+        }
+    }
+}
+
+// Row blocks of 16 that a wave holds.
+int row_blocks(const qnn_attention_params &p, int group) { return (int64_t)p.max_q * group <= 16 ? 1 : 2; }
+
+template <int DP>
+hipError_t launch_attention(const AttnArgs &a, int blocks, hipStream_t st)
+{
+    const dim3 grid((unsigned)((a.total + 7) / 8 * 8)), block(kWaves * 64);
+    if (blocks == 1)
+        launch_main((attention4_kernel<DP, 1>), grid, block, 0, st, a);
+    else
+        launch_main((attention4_kernel<DP, 2>), grid, block, 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace qnn
+
+using namespace qnn;
+
+extern "C" {
+
+size_t qnn_attention4_workspace_size(qnn_cache4 cache, qnn_attention_params p)
+{
+    (void)cache;
+    (void)p;
+    return 0;
+}
+
+qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qparams q_q, qnn_cache4 cache,
+                          const int32_t *table, const int32_t *ctx, const int32_t *cu_q, qnn_attention_params p,
+                          void *o, qnn_dtype o_dtype, qnn_qparams o_q, void *workspace, size_t workspace_bytes)
+{
+    AttnArgs a{};
+    qnn_status s = check_cache4(cache, "attention4", &a.c);
+    if (s != QNN_OK)
+        return s;
+    auto whole = [](qnn_dtype t) { return t == QNN_UINT8 || t == QNN_INT8; };
+    auto known = [&](qnn_dtype t) { return whole(t) || t == QNN_FLOAT16 || t == QNN_BFLOAT16; };
+    if (!known(q_dtype) || !known(o_dtype))
+        return fail(QNN_ERR_DTYPE, "attention4: q and o must be uint8, int8, float16 or bfloat16");
+    if (p.tokens < 0 || p.requests < 0 || p.q_heads < 1 || p.max_q < 1 || p.max_ctx < 0 || p.window < 0)
+        return fail(QNN_ERR_SHAPE, "attention4: tokens %d, requests %d, q_heads %d, max_q %d, max_ctx %d, window %d",
+                    p.tokens, p.requests, p.q_heads, p.max_q, p.max_ctx, p.window);
+    if (p.q_heads % a.c.heads)
+        return fail(QNN_ERR_SHAPE, "attention4: %d query heads over %d cache heads", p.q_heads, a.c.heads);
+    if (p.table_width < 1 || p.table_ld < p.table_width || (int64_t)p.table_width * cache.page_size >= (int64_t(1) << 31))
+        return fail(QNN_ERR_SHAPE, "attention4: table_width %d, table_ld %lld", p.table_width, (long long)p.table_ld);
+    const int64_t row = (int64_t)p.q_heads * a.c.dim;
+    if (p.q_ld < row || p.o_ld < row)
+        return fail(QNN_ERR_SHAPE, "attention4: row strides %lld and %lld do not hold %d heads of %d", (long long)p.q_ld,
+                    (long long)p.o_ld, p.q_heads, a.c.dim);
+    if (!cu_q && p.tokens != p.requests)
+        return fail(QNN_ERR_SHAPE, "attention4: %d tokens of %d requests need cu_q", p.tokens, p.requests);
+    if (!std::isfinite(p.scale))
+        return fail(QNN_ERR_QPARAM, "attention4: scale is not finite");
+    if (whole(q_dtype) && (s = check_qparams(q_q, "q qparams", 1, q_dtype, false)) != QNN_OK)
+        return s;
+    if (whole(o_dtype) && (s = check_qparams(o_q, "o qparams", 1, o_dtype, false)) != QNN_OK)
+        return s;
+    if (p.tokens == 0 || p.requests == 0)
+        return QNN_OK;
+    if (!q || !o || !table || !ctx)
+        return fail(QNN_ERR_NULL, "attention4: q, o, table or ctx is NULL");
+    const int q_size = whole(q_dtype) ? 1 : 2, o_size = whole(o_dtype) ? 1 : 2;
+    if (p.q_ld % 8 || p.o_ld % 8 || ((uintptr_t)q & (8 * q_size - 1)) || ((uintptr_t)o & (8 * o_size - 1)))
+        return fail(QNN_ERR_UNSUPPORTED, "attention4: rows of q and o must be aligned to 8 elements");
+    if (qnn_attention4_workspace_size(cache, p) > workspace_bytes)
+        return fail(QNN_ERR_SHAPE, "attention4: the workspace is smaller than qnn_attention4_workspace_size()");
+    (void)workspace;
+    a.q = q;
+    a.o = o;
+    a.table = table;
+    a.ctx = ctx;
+    a.cu = cu_q;
+    a.q_ld = p.q_ld;
+    a.o_ld = p.o_ld;
+    a.table_ld = p.table_ld;
+    a.q_dt = q_dtype;
+    a.o_dt = o_dtype;
+    a.tokens = p.tokens;
+    a.requests = p.requests;
+    a.q_heads = p.q_heads;
+    a.group = p.q_heads / a.c.heads;
+    a.width = p.table_width;
+    a.max_q = cu_q ? p.max_q : 1;
+    a.causal = p.causal != 0;
+    a.window = p.window;
+    a.scale = p.scale * 1.44269504088896340736f * (whole(q_dtype) ? q_q.scale[0] : 1.0f);
+    a.q_zp = whole(q_dtype) ? q_q.zero_point[0] : 0;
+    if (whole(o_dtype)) {
+        Range r;
+        dtype_range(o_dtype, &r);
+        a.o_scale = o_q.scale[0];
+        a.o_zp = o_q.zero_point[0];
+        a.o_lo = (int32_t)r.lo;
+        a.o_hi = (int32_t)r.hi;
+    }
+    const int blocks = row_blocks(p, a.group);
+    const int64_t tiles = ((int64_t)a.max_q * a.group + 16 * blocks - 1) / (16 * blocks);
+    const int64_t total = tiles * a.c.heads * p.requests;
+    if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || total >= (int64_t(1) << 31) - 8)
+        return fail(QNN_ERR_UNSUPPORTED, "attention4: too many row tiles");
+    a.tiles = (int32_t)tiles;
+    a.total = (int32_t)total;
+    const int dp = cache4_padded(a.c.dim);
+    const hipStream_t st = (hipStream_t)stream;
+    const hipError_t e = dp == 64    ? launch_attention<64>(a, blocks, st)
+                         : dp == 128 ? launch_attention<128>(a, blocks, st)
+                                     : launch_attention<256>(a, blocks, st);
+    return e == hipSuccess ? QNN_OK : hip_fail(e, "attention4 launch");
+}
+
+}  // extern "C"

@@ -2,6 +2,7 @@
 // fixed-point multipliers, folded constants, packed weights), kernel choice
 // and launches.  See include/qnn.h for the contract of every entry point.
 #include "qnn.h"
+#include "qnn_host.h"
 #include "qnn_internal.h"
 
 #include <algorithm>
@@ -25,9 +26,9 @@ qnn::LaunchEvents &qnn::launch_events()
     return ev;
 }
 
-namespace {
+namespace qnn {
 
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 qnn_status fail(qnn_status s, const char *fmt, ...)
 {
@@ -44,17 +45,6 @@ qnn_status hip_fail(hipError_t e, const char *what)
 {
     return fail(QNN_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
-
-#define HIP_TRY(expr)                                 \
-    do {                                              \
-        hipError_t e_ = (expr);                       \
-        if (e_ != hipSuccess)                         \
-            return hip_fail(e_, #expr);               \
-    } while (0)
-
-struct Range {
-    int64_t lo, hi;
-};
 
 bool dtype_range(qnn_dtype t, Range *r)
 {
@@ -78,7 +68,7 @@ const char *dtype_name(qnn_dtype t)
 
 // Fixed-point multiplier of Sec. III-B (the library's own derivation; see
 // qnn_quantize_multiplier in qnn.h for the rule).
-bool derive_multiplier(double M, int32_t *mult, int32_t *shift)
+static bool derive_multiplier(double M, int32_t *mult, int32_t *shift)
 {
     if (!(M >= 0.0) || !std::isfinite(M))
         return false;
@@ -135,6 +125,25 @@ qnn_status out_bounds(qnn_dtype yt, qnn_clamp act, int32_t *lo, int32_t *hi)
     *hi = (int32_t)h;
     return QNN_OK;
 }
+
+// Compute units of the current device.
+int device_cus()
+{
+    static int cus = 0;
+    if (!cus) {
+        int dev = 0, n = 0;
+        if (hipGetDevice(&dev) == hipSuccess &&
+            hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
+            cus = n;
+        else
+            cus = 256;
+    }
+    return cus;
+}
+
+}  // namespace qnn
+
+namespace {
 
 int env_int(const char *name, int dflt)
 {
@@ -329,7 +338,6 @@ TileShape kernel_shape(const ConvKernel &k)
     }
 }
 
-int device_cus();
 int device_lds_per_block();
 
 // Candidate kernels for a conv of M pixels x K channels with C4 channels
@@ -881,20 +889,6 @@ int device_lds_per_block()
             bytes = 64 * 1024;
     }
     return bytes;
-}
-
-int device_cus()
-{
-    static int cus = 0;
-    if (!cus) {
-        int dev = 0, n = 0;
-        if (hipGetDevice(&dev) == hipSuccess &&
-            hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
-            cus = n;
-        else
-            cus = 256;
-    }
-    return cus;
 }
 
 // ---- depthwise 3x3 kernel configurations

@@ -22,7 +22,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libqnn.so")
 
-UINT8, INT8, INT32 = 0, 1, 2
+UINT8, INT8, INT32, FLOAT16, BFLOAT16 = 0, 1, 2, 3, 4
 HALF_UP, HALF_AWAY, TWO_STAGE = 0, 1, 2
 _TORCH_DT = {torch.uint8: UINT8, torch.int8: INT8, torch.int32: INT32}
 _NAME_DT = {"u8": UINT8, "i8": INT8, "i32": INT32}
@@ -38,6 +38,8 @@ EXPORTS = [
     "qnn_abi_version", "qnn_last_error", "qnn_status_string", "qnn_quantize_multiplier",
     "qnn_conv2d", "qnn_depthwise_conv2d", "qnn_dense", "qnn_requantize", "qnn_add",
     "qnn_pool2d",
+    "qnn_cache4_page_bytes", "qnn_cache4_append", "qnn_cache4_read", "qnn_attention4_workspace_size",
+    "qnn_attention4", "qnn_pages_workspace_size", "qnn_pages_resize",
     "qnn_conv2d_plan_create", "qnn_depthwise_conv2d_plan_create", "qnn_dense_plan_create",
     "qnn_conv2d_plan_create_wt", "qnn_depthwise_conv2d_plan_create_wt", "qnn_dense_plan_create_wt",
     "qnn_requantize_plan_create", "qnn_plan_run", "qnn_plan_run_timed", "qnn_time_next_kernel", "qnn_plan_run_noalloc",
@@ -66,6 +68,16 @@ class ConvParams(ctypes.Structure):
 
 class Clamp(ctypes.Structure):
     _fields_ = [("lo", ctypes.c_int32), ("hi", ctypes.c_int32)]
+
+
+class Cache4Desc(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("pages", "page_size", "heads", "head_dim")]
+
+
+class AttentionParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("tokens", "q_heads", "requests", "table_width")] +
+                [(n, ctypes.c_int64) for n in ("q_ld", "o_ld", "table_ld")] +
+                [(n, ctypes.c_int32) for n in ("max_q", "max_ctx", "causal", "window")] + [("scale", ctypes.c_float)])
 
 
 _lib = None
@@ -102,6 +114,21 @@ def lib() -> ctypes.CDLL:
     L.qnn_add.restype = st
     L.qnn_pool2d.argtypes = [P, P, st, i32, i32, i32, i32, i32, i32, ConvParams, st, i32, i32, P, st]
     L.qnn_pool2d.restype = st
+    L.qnn_cache4_page_bytes.argtypes = [i32, i32, i32]
+    L.qnn_cache4_page_bytes.restype = ctypes.c_size_t
+    L.qnn_cache4_append.argtypes = [P, Cache4Desc, P, P, st, QParams, QParams, i32, i64, i64, P]
+    L.qnn_cache4_append.restype = st
+    L.qnn_cache4_read.argtypes = [P, Cache4Desc, P, i32, P, P, st, i64, i64]
+    L.qnn_cache4_read.restype = st
+    L.qnn_attention4_workspace_size.argtypes = [Cache4Desc, AttentionParams]
+    L.qnn_attention4_workspace_size.restype = ctypes.c_size_t
+    L.qnn_attention4.argtypes = [P, P, st, QParams, Cache4Desc, P, P, P, AttentionParams, P, st, QParams, P,
+                                 ctypes.c_size_t]
+    L.qnn_attention4.restype = st
+    L.qnn_pages_workspace_size.argtypes = [i32]
+    L.qnn_pages_workspace_size.restype = ctypes.c_size_t
+    L.qnn_pages_resize.argtypes = [P, i32, i32, P, P, P, i32, i64, P, i32, P, P, P, P, i32, P, P]
+    L.qnn_pages_resize.restype = st
     PP = ctypes.POINTER(ctypes.c_void_p)
     L.qnn_conv2d_plan_create.argtypes = [PP, P, st, i32, i32, i32, i32, QParams, P, i32, i32, i32,
                                          QParams, P, ConvParams, st, QParams, Clamp, st, i32, i32]
@@ -591,3 +618,208 @@ def pool2d(x: torch.Tensor, mode="avg", kernel=(3, 3), stride=(1, 1), pads=0, co
     _check(lib().qnn_pool2d(_stream(stream), _ptr(x), _dt(x), N, H, W, C, R, S, cp, _POOL_MODE[mode],
                             int(bool(count_pad)), int(zp), _ptr(out), _ROUND[rounding]))
     return out
+
+
+# ---------------------------------------------------------------- 4-bit cache
+
+# Element types of the cache's operators; those above stay with whole numbers.
+_FLOAT_DT = {**{k: v for k, v in _TORCH_DT.items() if k != torch.int32},
+             torch.float16: FLOAT16, torch.bfloat16: BFLOAT16}
+_FLOAT_NAME = {"u8": torch.uint8, "i8": torch.int8, "f16": torch.float16, "bf16": torch.bfloat16}
+_NO_Q = QParams(None, None, 0)
+
+
+def _here(device: torch.device, **tensors):
+    """Every given tensor on `device`, which must be the current one."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {device}, the current device is cuda:{torch.cuda.current_device()}"
+                         if device.type == "cuda" else "the tensors must be device tensors")
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _ints(t: Optional[torch.Tensor], name: str, count: Optional[int] = None):
+    """A contiguous int32 vector (of `count` entries)."""
+    if t is None:
+        return
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (count is not None and t.numel() != count):
+        raise ValueError(f"{name} must be a contiguous int32 vector" + ("" if count is None else f" of {count} entries")
+                         + f", not {tuple(t.shape)} {t.dtype}")
+
+
+def _heads(t: torch.Tensor, name: str, shape) -> int:
+    """Row stride of a [tokens][heads][head_dim] tensor whose rows are contiguous."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
+    T, H, D = t.shape
+    if D > 1 and t.stride(2) != 1 or H > 1 and t.stride(1) != D:
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    if T > 1 and t.stride(0) < H * D:
+        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)})")
+    return t.stride(0) if T > 1 else max(H * D, t.stride(0))
+
+
+def _table(t: torch.Tensor, rows: int) -> int:
+    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"the block table must be int32 [{rows}][pages] with contiguous rows, not {tuple(t.shape)} "
+                         f"{t.dtype}")
+    if rows > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"the block table's rows overlap (stride {t.stride(0)})")
+    return t.stride(0) if rows > 1 else t.shape[1]
+
+
+class Cache4:
+    """Keys and values of an attention as 4-bit codes, in pages (qnn_cache4):
+    `data` is a uint8 tensor [num_pages][bytes of a page], allocated here unless
+    given."""
+
+    def __init__(self, num_pages: int, page_size: int, heads: int, head_dim: int, device="cuda",
+                 data: Optional[torch.Tensor] = None):
+        per_page = int(lib().qnn_cache4_page_bytes(page_size, heads, head_dim))
+        if per_page == 0 or num_pages < 1:
+            raise ValueError(f"no cache of {num_pages} pages of {page_size} tokens, {heads} heads of {head_dim}: "
+                             "page_size is 16, 32, 64, 128 or 256, head_dim a multiple of 8 up to 256")
+        if data is None:
+            data = torch.empty((num_pages, per_page), dtype=torch.uint8, device=device)
+        if data.dtype != torch.uint8 or tuple(data.shape) != (num_pages, per_page) or not data.is_contiguous():
+            raise ValueError(f"data must be contiguous uint8 {(num_pages, per_page)}, not {tuple(data.shape)} "
+                             f"{data.dtype}")
+        if not data.is_cuda:
+            raise ValueError("data must be a device tensor")
+        self.data, self.num_pages, self.page_size = data, num_pages, page_size
+        self.heads, self.head_dim = heads, head_dim
+        self.desc = Cache4Desc(data.data_ptr(), num_pages, page_size, heads, head_dim)
+
+
+def cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_scale=1.0, k_zp=0,
+                  v_scale=1.0, v_zp=0, stream=None) -> None:
+    """Quantizes k and v ([tokens][heads][head_dim], f16, bf16, or u8 / i8 with
+    their scale and zero point) to 4 bits at `slots` (int32; below 0: skipped);
+    see qnn_cache4_append.  k and v may be slices of a wider tensor of rows."""
+    T = k.shape[0]
+    _here(cache.data.device, k=k, v=v, slots=slots)
+    if k.dtype not in _FLOAT_DT or v.dtype != k.dtype:
+        raise TypeError(f"k and v must both be f16, bf16, u8 or i8, not {k.dtype} and {v.dtype}")
+    k_ld, v_ld = (_heads(t, n, (T, cache.heads, cache.head_dim)) for t, n in ((k, "k"), (v, "v")))
+    _ints(slots, "slots", T)
+    whole = k.dtype in (torch.uint8, torch.int8)
+    kq, vq = (_Q(k_scale, k_zp, 1), _Q(v_scale, v_zp, 1)) if whole else (None, None)
+    status = lib().qnn_cache4_append(_stream_handle(stream), cache.desc, k.data_ptr(), v.data_ptr(),
+                                     _FLOAT_DT[k.dtype], kq.q if whole else _NO_Q, vq.q if whole else _NO_Q, T, k_ld,
+                                     v_ld, slots.data_ptr())
+    if status:
+        _check(status)
+
+
+def cache4_read(cache: Cache4, slots: torch.Tensor, dtype="f16", stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(k, v) at `slots` as [slots][heads][head_dim] of dtype "f16" or "bf16";
+    slots outside the cache give zeros.  See qnn_cache4_read."""
+    _here(cache.data.device, slots=slots)
+    _ints(slots, "slots")
+    T = slots.numel()
+    dt = _FLOAT_NAME[dtype]
+    k, v = torch.empty((2, T, cache.heads, cache.head_dim), dtype=dt, device=cache.data.device).unbind(0)
+    ld = cache.heads * cache.head_dim
+    status = lib().qnn_cache4_read(_stream_handle(stream), cache.desc, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(),
+                                   _FLOAT_DT[dt], ld, ld)
+    if status:
+        _check(status)
+    return k, v
+
+
+def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: torch.Tensor,
+               cu_q: Optional[torch.Tensor] = None, max_q: int = 1, max_ctx: int = 0, scale: Optional[float] = None,
+               causal=True, window: int = 0, q_scale=1.0, q_zp=0, y_scale=1.0, y_zp=0, y_dtype: Optional[str] = None,
+               out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """Attention of q ([tokens][q_heads][head_dim], f16, bf16, or u8 / i8 with
+    q_scale and q_zp) over the cache; see qnn_attention4.  Request b's queries
+    are rows cu_q[b] .. cu_q[b + 1] - 1 (cu_q None: one each), the last of its
+    ctx[b] tokens; block_table is int32 [requests][pages].  max_q is at least any
+    request's queries, max_ctx (0: unknown) about the longest ctx.  scale
+    defaults to head_dim ** -0.5.  The output has y_dtype ("f16", "bf16", "u8",
+    "i8"; q's by default), 8-bit ones with y_scale and y_zp.  `workspace` is a
+    uint8 tensor of attention4_workspace_size() bytes, allocated here if not
+    given; two calls that may overlap need one each."""
+    if q.dim() != 3:
+        raise ValueError("q must be [tokens][heads][head_dim]")
+    T, Hq, D = q.shape
+    B = ctx.numel()
+    _here(cache.data.device, q=q, block_table=block_table, ctx=ctx, cu_q=cu_q, out=out, workspace=workspace)
+    if q.dtype not in _FLOAT_DT:
+        raise TypeError(f"q must be f16, bf16, u8 or i8, not {q.dtype}")
+    _ints(ctx, "ctx")
+    _ints(cu_q, "cu_q", B + 1)
+    q_ld = _heads(q, "q", (T, Hq, cache.head_dim))
+    odt = q.dtype if y_dtype is None else _FLOAT_NAME[y_dtype]
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=odt, device=q.device)
+    if out.dtype != odt:
+        raise ValueError(f"out is {out.dtype}, not {odt}")
+    p = AttentionParams(T, Hq, B, block_table.shape[1] if block_table.dim() == 2 else 0, q_ld,
+                        _heads(out, "out", (T, Hq, D)), _table(block_table, B), max_q, max_ctx, int(bool(causal)),
+                        window, D ** -0.5 if scale is None else scale)
+    need = lib().qnn_attention4_workspace_size(cache.desc, p)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    have = 0
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        have = workspace.numel() * workspace.element_size()
+    qq = _Q(q_scale, q_zp, 1) if q.dtype in (torch.uint8, torch.int8) else None
+    oq = _Q(y_scale, y_zp, 1) if odt in (torch.uint8, torch.int8) else None
+    status = lib().qnn_attention4(_stream_handle(stream), q.data_ptr(), _FLOAT_DT[q.dtype], qq.q if qq else _NO_Q,
+                                  cache.desc, block_table.data_ptr(), ctx.data_ptr(),
+                                  None if cu_q is None else cu_q.data_ptr(), p, out.data_ptr(), _FLOAT_DT[odt],
+                                  oq.q if oq else _NO_Q, None if workspace is None else workspace.data_ptr(), have)
+    if status:
+        _check(status)
+    return out
+
+
+def attention4_workspace_size(cache: Cache4, tokens: int, q_heads: int, requests: int, table_width: int,
+                              max_q: int = 1, max_ctx: int = 0, causal=True, window: int = 0) -> int:
+    """Bytes of workspace of attention4 calls of these sizes (0: none)."""
+    ld = q_heads * cache.head_dim
+    p = AttentionParams(tokens, q_heads, requests, table_width, ld, ld, table_width, max_q, max_ctx, int(bool(causal)),
+                        window, 1.0)
+    return int(lib().qnn_attention4_workspace_size(cache.desc, p))
+
+
+def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
+                 free_count: torch.Tensor, page_size: int, token_capacity: int,
+                 workspace: Optional[torch.Tensor] = None, stream=None):
+    """Resizes requests of lens[b] tokens to new_lens[b]: block_table, lens, and
+    the free stack (free_pages, free_count[0]) are updated, and every new token
+    gets a slot; see qnn_pages_resize.  Returns (cu, slots, positions, status):
+    request b's new tokens are slots[cu[b]:cu[b + 1]], unused entries -1; status
+    (a device int32) is 0, or says why nothing was changed.  All arguments are
+    int32 device tensors."""
+    B = lens.numel()
+    dev = lens.device
+    _here(dev, new_lens=new_lens, block_table=block_table, free_pages=free_pages, free_count=free_count,
+          workspace=workspace)
+    _ints(lens, "lens")
+    _ints(new_lens, "new_lens", B)
+    _ints(free_pages, "free_pages")
+    _ints(free_count, "free_count", 1)
+    ld = _table(block_table, B)
+    need = int(lib().qnn_pages_workspace_size(B))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    elif not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
+        raise ValueError("workspace must be contiguous and of qnn_pages_workspace_size() bytes")
+    if token_capacity < 0:
+        raise ValueError("token_capacity must be >= 0")
+    out = torch.empty(B + 2 + 2 * token_capacity, dtype=torch.int32, device=dev)
+    cu, status = out[:B + 1], out[B + 1:B + 2]
+    slots, positions = out[B + 2:B + 2 + token_capacity], out[B + 2 + token_capacity:]
+    code = lib().qnn_pages_resize(_stream_handle(stream), B, page_size, lens.data_ptr(), new_lens.data_ptr(),
+                                  block_table.data_ptr(), block_table.shape[1], ld, free_pages.data_ptr(),
+                                  free_pages.numel(), free_count.data_ptr(), cu.data_ptr(), slots.data_ptr(),
+                                  positions.data_ptr(), token_capacity, status.data_ptr(), workspace.data_ptr())
+    if code:
+        _check(code)
+    return cu, slots, positions, status
