@@ -558,6 +558,52 @@ qnn_status qnn_plan_set_residual(qnn_plan *plan, qnn_dtype r_dtype, qnn_qparams 
                                  qnn_rounding rounding);
 
 /*
+ * Activation by table in a matrix product's epilogue.  A function of an 8-bit
+ * quantized tensor is 256 bytes: after the call the plan stores
+ *   y = table[c]
+ * where c is the output byte exactly as the plan computed it (y_dtype, y_q,
+ * act, rounding of the plan; int8 as its two's complement byte), never written,
+ * and y is of y_dtype (UINT8 / INT8) with the per-tensor y_q: the operand and
+ * qparams of a qnn_plan_set_residual that follows (y = qnn_add(table[c], r)).
+ * The bytes equal those of qnn_plan_run followed by qnn_lookup.  `table` is a
+ * host array of 256 bytes, copied to device memory of the plan here (waits for
+ * the copy); qnn_activation_table makes it.
+ * Plans of matrix products (dense, and conv2d with a 1x1 filter and no padding)
+ * with 8-bit outputs on the short-loop and few-pixel kernels
+ * (qnn_plan_describe starting with "conv_dma_flow" or "conv_dma_small", as
+ * every such plan does unless a choice is forced or recorded otherwise) accept
+ * it; others, and plans with an activation or a residual already, return
+ * QNN_ERR_UNSUPPORTED and stay as they were: qnn_lookup does the same in a pass
+ * of its own.
+ */
+qnn_status qnn_plan_set_activation(qnn_plan *plan, const uint8_t *table, qnn_dtype y_dtype, qnn_qparams y_q);
+
+typedef enum QNN_ENUM_INT {
+    QNN_ACT_GELU = 0,        /* x (1 + erf(x / sqrt 2)) / 2 */
+    QNN_ACT_GELU_TANH = 1,   /* its tanh form: x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
+    QNN_ACT_SILU = 2,        /* x / (1 + e^-x) */
+    QNN_ACT_SIGMOID = 3,
+    QNN_ACT_TANH = 4,
+    QNN_ACT_HARD_SWISH = 5   /* x min(max(x + 3, 0), 6) / 6 */
+} qnn_activation;
+
+/*
+ * The table of an activation f between quantized tensors:
+ *   table[b] = clamp(zp_y + round(f(s_x * (b - zp_x)) / s_y))
+ * for every byte b read as x_dtype (UINT8 / INT8), in double precision, ties
+ * away from zero; x_q, y_q per tensor.  Pure host function, no device work.
+ */
+qnn_status qnn_activation_table(qnn_activation kind, qnn_dtype x_dtype, qnn_qparams x_q, qnn_dtype y_dtype,
+                                qnn_qparams y_q, uint8_t *table);
+
+/*
+ * y[i] = table[x[i]]: x and y are device arrays of `count` bytes (the same
+ * array, or not overlapping), `table` a host array of 256 bytes.  Enqueued on
+ * `stream`, no synchronization.
+ */
+qnn_status qnn_lookup(void *stream, const void *x, const uint8_t *table, int64_t count, void *y);
+
+/*
  * Runs a plan with a fused residual add: as qnn_plan_run, with the
  * residual device buffer (layout set by qnn_plan_set_residual, not
  * overlapping y).  y must be 16-byte aligned (QNN_ERR_UNSUPPORTED, nothing

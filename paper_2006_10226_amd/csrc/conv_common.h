@@ -235,12 +235,54 @@ __device__ __forceinline__ lds_i32 *fuse_tables()
     }
 }
 
+// Activation of requantized bytes by table (ConvArgs::act). The 256 bytes are
+// one dword in each of the LDS's 64 banks, so 64 lanes reading any bytes of them
+// never conflict; an element is a read and two or three instructions, whatever
+// the function: dense 8192 x 4096 x 4096 with SiLU and a residual 252 us.
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
+// LDS home of the table in the instantiations that have an activation.
+template <bool ACT>
+__device__ __forceinline__ lds_u8 *act_table()
+{
+    if constexpr (ACT) {
+        __shared__ __attribute__((aligned(16))) uint8_t tab[256];
+        return (lds_u8 *)tab;
+    } else {
+        return nullptr;
+    }
+}
+
+// Brings the table there: one LDS-direct load of a wave, older than the wave's
+// other loads, so that its later waits cover it.
+template <bool ACT>
+__device__ __forceinline__ void load_act_table(const ConvArgs &a)
+{
+    if constexpr (ACT) {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)a.act, (short)0, 256, kBufFlags);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)act_table<ACT>(), 4,
+                                                 (int)(threadIdx.x & 63) * 4, 0, 0, 0);
+    }
+}
+
+__device__ __forceinline__ uint32_t act4(uint32_t v, const lds_u8 *tab)
+{
+    return (uint32_t)tab[v & 0xffu] | (uint32_t)tab[(v >> 8) & 0xffu] << 8 | (uint32_t)tab[(v >> 16) & 0xffu] << 16 |
+           (uint32_t)tab[v >> 24] << 24;
+}
+
+__device__ __forceinline__ v4i act16(v4i v, const lds_u8 *tab)
+{
+    return v4i{(int)act4((uint32_t)v[0], tab), (int)act4((uint32_t)v[1], tab), (int)act4((uint32_t)v[2], tab),
+               (int)act4((uint32_t)v[3], tab)};
+}
+
 // Copy-out of a staged tile (TP pixel rows of SP bytes in LDS, the tile's
 // first min(TC, kmax) channels valid) with the residual add applied, the
 // residual chunks prefetched in r (byte loads here where they were not);
 // the f32 form where the plan has one, else tab: the term tables in LDS, or
 // nullptr for the add's own arithmetic.
-template <int TC, int TP, int NT, int SP>
+template <int TC, int TP, int NT, int SP, bool ACT = false>
 __device__ __forceinline__ void copy_out_residual(const ConvArgs &a, const int8_t *stage, int c0, int p0, int kmax,
                                                   const v4i (&r)[(TP * (TC / 16) + NT - 1) / NT],
                                                   const lds_i32 *tab)
@@ -263,7 +305,9 @@ __device__ __forceinline__ void copy_out_residual(const ConvArgs &a, const int8_
                         w[e >> 2] |= (uint32_t)rp[e] << (8 * (e & 3));
                 rv = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
             }
-            const v4i sv = *(const v4i *)(stage + pl * SP + qc * 16);
+            v4i sv = *(const v4i *)(stage + pl * SP + qc * 16);
+            if constexpr (ACT)
+                sv = act16(sv, act_table<ACT>());
             const v4i v = a.fadd.flt ? residual_add16_f32(a, sv, rv)
                           : tab      ? residual_add16_tab(a, sv, rv, tab)
                                      : residual_add16(a, sv, rv);
@@ -376,8 +420,10 @@ __device__ __forceinline__ void add_bconst(v4i (&acc)[TC / WC / 16][TP / WP / 16
 // instantiations only without either; the largest wave tiles have no
 // registers for them).
 // KREC: recs holds the records of requant4_rec, and the accumulators don't
-// hold bconst.
-template <int TC, int TP, int WC, int WP, int STAGE_BYTES, bool FUSE = false, bool PLAIN = false, bool KREC = false>
+// hold bconst.  ACT: the requantized bytes go through the table that the
+// kernel has brought to act_table (load_act_table, and the waits that cover recs).
+template <int TC, int TP, int WC, int WP, int STAGE_BYTES, bool FUSE = false, bool PLAIN = false, bool KREC = false,
+          bool ACT = false>
 __device__ __forceinline__ void store_tile(const ConvArgs &a, v4i (&acc)[TC / WC / 16][TP / WP / 16], int8_t *stage,
                                            int c0, int p0, const ChanRec *recs)
 {
@@ -480,7 +526,7 @@ __device__ __forceinline__ void store_tile(const ConvArgs &a, v4i (&acc)[TC / WC
         constexpr int CH = TC / 16;
         const int kmax = a.K - c0;
         if constexpr (FUSE) {
-            copy_out_residual<TC, TP, NT, SP>(a, stage, c0, p0, kmax, rres,
+            copy_out_residual<TC, TP, NT, SP, ACT>(a, stage, c0, p0, kmax, rres,
                                               a.fadd.tab ? fuse_tables<FUSE>() : nullptr);
             return;
         }
@@ -491,7 +537,9 @@ __device__ __forceinline__ void store_tile(const ConvArgs &a, v4i (&acc)[TC / WC
                 const int pl = idx / CH, qc = idx % CH;
                 const int m = p0 + pl;
                 if (m < a.M && qc * 16 < kmax) {
-                    const v4i v = *(const v4i *)(stage + pl * SP + qc * 16);
+                    v4i v = *(const v4i *)(stage + pl * SP + qc * 16);
+                    if constexpr (ACT)
+                        v = act16(v, act_table<ACT>());
                     uint8_t *dst = (uint8_t *)a.y + (size_t)m * a.y_ldc + a.y_coff + c0 + qc * 16;
                     if (qc * 16 + 16 <= kmax) {
                         __builtin_nontemporal_store(v, (v4i *)dst);
@@ -543,6 +591,8 @@ __device__ __forceinline__ void store_tile(const ConvArgs &a, v4i (&acc)[TC / WC
                                 : requant4_rec<Req::CHAN>(a, acc[i][j], rec);
             else
                 packed = requant4(a, acc[i][j], rec);
+            if constexpr (ACT)
+                packed = act4(packed, act_table<ACT>());
             uint8_t *yp = (uint8_t *)a.y + off;
             if (full) {
                 __builtin_nontemporal_store(packed, (uint32_t *)yp);

@@ -22,6 +22,8 @@ size_t flow_lds_bytes(int tile, int nk, bool linear)
 
 hipError_t launch_conv_flow(const ConvArgs &a, int tile, hipStream_t st)
 {
+    if (a.act)
+        return a.res ? launch_conv_flow_act_fused(a, tile, st) : launch_conv_flow_act(a, tile, st);
     return a.res ? launch_conv_flow_fused(a, tile, st) : launch_flow_from<0, false>(a, tile, st);
 }
 

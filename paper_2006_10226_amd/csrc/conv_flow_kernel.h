@@ -108,8 +108,9 @@ constexpr int flow_occupancy()
 // TC x TP tile on WC x WP waves (times KS groups that take alternate K-steps
 // of the same tile, each through its own ring of NS / KS stages; the second
 // group's sums are added through LDS).  SHORT: at most NS K-steps, all in
-// flight at once, no ring.  FUSE: the epilogue applies the residual add.
-template <int TC, int TP, int WC, int WP, int NS, int KS, bool SHORT, bool TAB, bool FLIP, bool FUSE>
+// flight at once, no ring.  FUSE: the epilogue applies the residual add; ACT: the
+// activation by table.
+template <int TC, int TP, int WC, int WP, int NS, int KS, bool SHORT, bool TAB, bool FLIP, bool FUSE, bool ACT = false>
 __global__ void __launch_bounds__(WC *WP * 64 * KS, (flow_occupancy<TC / WC, TP / WP, WC *WP * 64 * KS>()))
     conv_flow_kernel(ConvArgs a)
 {
@@ -174,6 +175,7 @@ __global__ void __launch_bounds__(WC *WP * 64 * KS, (flow_occupancy<TC / WC, TP 
     if (grp == 0 && wave == NW - 1) {
         // the tile's channel records, a kilobyte per load; older than this
         // wave's stage loads, so every stage wait covers them
+        load_act_table<ACT>(a);
         const __amdgpu_buffer_rsrc_t rc =
             __builtin_amdgcn_make_buffer_rsrc(a.krec ? (void *)a.krec : (void *)a.chan, (short)0, a.Kpad * (int)sizeof(ChanRec), kBufFlags);
 #pragma unroll
@@ -470,7 +472,7 @@ __global__ void __launch_bounds__(WC *WP * 64 * KS, (flow_occupancy<TC / WC, TP 
             __syncthreads();   // every partial read before the staging overwrites them
         }
     }
-    store_tile<TC, TP, WC, WP, LDS_BYTES, FUSE, BIG, true>(a, acc, lds, c0, p0, recs);
+    store_tile<TC, TP, WC, WP, LDS_BYTES, FUSE, BIG, true, ACT>(a, acc, lds, c0, p0, recs);
 }
 
 // FlowTile -> tile, wave grid, stages, K-step groups, short form.
@@ -540,6 +542,39 @@ hipError_t launch_flow_from(const ConvArgs &a, int tile, hipStream_t st)
         return hipErrorInvalidValue;
     }
 }
+
+// The same with an activation by table: matrix products only (a.linear), the
+// form that needs no chunk table.
+template <int T, bool FUSE>
+hipError_t launch_flow_act_from(const ConvArgs &a, int tile, hipStream_t st)
+{
+    if constexpr (T < FLOW_COUNT) {
+        if (tile != T)
+            return launch_flow_act_from<T + 1, FUSE>(a, tile, st);
+        constexpr FlowCfg c = kFlowCfg[T];
+        if constexpr (FUSE && !flow_fuse_cfg(T)) {
+            return hipErrorInvalidValue;   // no fused-add instantiation
+        } else {
+            constexpr bool big = c.tc / c.wc * (c.tp / c.wp) >= 128 * 64;   // without term 3 only
+            if (!a.linear || a.mode != OUT_REQUANT || (c.sh && a.nk > c.ns) || (big && (a.asum || a.pcorr)))
+                return hipErrorInvalidValue;
+            const dim3 grid((a.ntiles + 7) / 8 * 8), block(c.wc * c.wp * 64 * c.ks);
+            if (a.flip4)
+                launch_main((conv_flow_kernel<c.tc, c.tp, c.wc, c.wp, c.ns, c.ks, c.sh, false, true, FUSE, true>), grid,
+                            block, 0, st, a);
+            else
+                launch_main((conv_flow_kernel<c.tc, c.tp, c.wc, c.wp, c.ns, c.ks, c.sh, false, false, FUSE, true>), grid,
+                            block, 0, st, a);
+            return hipGetLastError();
+        }
+    } else {
+        return hipErrorInvalidValue;
+    }
+}
+
+// Launches with an activation (a.act set), and with the residual add as well.
+hipError_t launch_conv_flow_act(const ConvArgs &a, int tile, hipStream_t st);
+hipError_t launch_conv_flow_act_fused(const ConvArgs &a, int tile, hipStream_t st);
 
 // Launch with the residual add fused (a.res set, a.staged).
 hipError_t launch_conv_flow_fused(const ConvArgs &a, int tile, hipStream_t st);

@@ -24,7 +24,8 @@ namespace qnn {
 constexpr int kSmallWaves = 8;
 
 // FC x FP blocks of 16 channels x 16 pixels per workgroup; TAB, FLIP as in
-// conv_flow_kernel; FUSE: the epilogue applies the residual add.
+// conv_flow_kernel; FUSE: the epilogue applies the residual add; ACT: the
+// activation by table.
 //
 // A load unit serves four neighbouring lanes at once if they read one 64-byte
 // run, and the MFMA wants neighbouring lanes in different rows. Weights are
@@ -33,7 +34,7 @@ constexpr int kSmallWaves = 8;
 // into the wave's own LDS and are read back in operand order, which needs no
 // barrier. Loading both straight in operand layout ran at a quarter of the
 // rate (15 bytes a clock per CU instead of 55; the 3x3 layer above 5.3 us).
-template <int FC, int FP, bool TAB, bool FLIP, bool FUSE>
+template <int FC, int FP, bool TAB, bool FLIP, bool FUSE, bool ACT = false>
 __global__ void __launch_bounds__(kSmallWaves * 64, 2) conv_small_kernel(ConvArgs a)
 {
     constexpr int NW = kSmallWaves, BK = 64;
@@ -61,6 +62,9 @@ __global__ void __launch_bounds__(kSmallWaves * 64, 2) conv_small_kernel(ConvArg
     const int ct = tile / tiles_p;
     const int c0 = ct * 16 * FC, p0 = (tile - ct * tiles_p) * 16 * FP;
     const int nk = a.nk;
+
+    if (wave == 0)
+        load_act_table<ACT>(a);   // the wave's own waits cover it, the barriers below the others
 
     // weights: block c0 / 16 + i of K-step s at ((c0 / 16 + i) * fJpad / 64 + s) KB
     int voffA[FC];
@@ -256,6 +260,8 @@ __global__ void __launch_bounds__(kSmallWaves * 64, 2) conv_small_kernel(ConvArg
             continue;
         }
         uint32_t packed = requant4(a, s, rec);
+        if constexpr (ACT)
+            packed = act4(packed, act_table<ACT>());
         if constexpr (FUSE) {
             if (a.fadd.flt) {
                 packed = residual_add4_f32(a, packed, res);
@@ -300,6 +306,13 @@ static hipError_t launch_small_cfg(const ConvArgs &a, hipStream_t st)
 {
     constexpr SmallCfg c = kSmallCfg[T];
     const dim3 grid((a.ntiles + 7) / 8 * 8), block(kSmallWaves * 64);
+    if (a.act) {
+        if (!a.linear || a.mode != OUT_REQUANT)
+            return hipErrorInvalidValue;
+        if (a.flip4) launch_main((conv_small_kernel<c.fc, c.fp, false, true, FUSE, true>), grid, block, 0, st, a);
+        else launch_main((conv_small_kernel<c.fc, c.fp, false, false, FUSE, true>), grid, block, 0, st, a);
+        return hipGetLastError();
+    }
     const uint32_t dyn = a.linear ? 0u : (uint32_t)((a.nk + 1) / 2) * 64u;
     if (a.linear && a.flip4) launch_main((conv_small_kernel<c.fc, c.fp, false, true, FUSE>), grid, block, dyn, st, a);
     else if (a.linear) launch_main((conv_small_kernel<c.fc, c.fp, false, false, FUSE>), grid, block, dyn, st, a);

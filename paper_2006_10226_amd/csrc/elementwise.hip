@@ -393,6 +393,50 @@ static void req_launch_y(const ReqArgs &a, int ydt, bool vec, hipStream_t s)
     else req_launch<XDT, 2>(a, vec, s);
 }
 
+// y = table[x]: the table's 256 bytes go to LDS, one dword per bank (reads never
+// conflict); VEC: 16 bytes a thread.
+template <bool VEC>
+__global__ void __launch_bounds__(256) lookup_kernel(LookupArgs a)
+{
+    __shared__ uint32_t tab[64];
+    if (threadIdx.x < 64)
+        tab[threadIdx.x] = a.table[threadIdx.x];
+    __syncthreads();
+    const uint8_t *const t = (const uint8_t *)tab;
+    const int64_t stride = (int64_t)gridDim.x * 256;
+    if constexpr (VEC) {
+        const int64_t n = a.count / 16;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
+            v4i v = *(const v4i *)(a.x + i * 16);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t u = (uint32_t)v[w];
+                v[w] = (int)((uint32_t)t[u & 0xffu] | (uint32_t)t[(u >> 8) & 0xffu] << 8 |
+                             (uint32_t)t[(u >> 16) & 0xffu] << 16 | (uint32_t)t[u >> 24] << 24);
+            }
+            *(v4i *)(a.y + i * 16) = v;
+        }
+        const int64_t rest = n * 16 + threadIdx.x;   // the last, partial 16
+        if (blockIdx.x == 0 && rest < a.count)
+            a.y[rest] = t[a.x[rest]];
+    } else {
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.count; i += stride)
+            a.y[i] = t[a.x[i]];
+    }
+}
+
+hipError_t launch_lookup(const LookupArgs &a, hipStream_t s)
+{
+    const bool vec = (((uintptr_t)a.x | (uintptr_t)a.y) & 15) == 0;
+    const int64_t items = vec ? (a.count + 15) / 16 : a.count;
+    const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 8192)));
+    if (vec)
+        launch_main((lookup_kernel<true>), grid, dim3(256), 0, s, a);
+    else
+        launch_main((lookup_kernel<false>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
 hipError_t launch_requantize(const ReqArgs &a, int xdt, int ydt, bool aligned, hipStream_t s)
 {
     if (xdt == 0) req_launch_y<0>(a, ydt, aligned, s);

@@ -178,6 +178,7 @@ struct qnn_plan {
     int y_dt = QNN_UINT8;
     bool fused = false;
     int32_t *addtab = nullptr;  // the fused add's term tables (AddArgs::tab), plan-owned
+    uint8_t *acttab = nullptr;  // the activation's table (ConvArgs::act), plan-owned
     size_t ws_asum_bytes = 0, ws_xpad_bytes = 0;
     size_t ws_cnt_bytes = 0, ws_part_bytes = 0;   // split reduction: counters, partial sums
     int32_t C_in = 0;           // channels of the caller's x (before padding to a.C)
@@ -210,6 +211,8 @@ void free_plan(qnn_plan *p)
         (void)hipFree(p->ws_own);
     if (p->addtab)
         (void)hipFree(p->addtab);
+    if (p->acttab)
+        (void)hipFree(p->acttab);
     delete p;
 }
 
@@ -2211,6 +2214,97 @@ static bool fit_float_term(bool is_int8, int32_t zp, int32_t mult, int32_t shift
             return true;
     }
     return false;
+}
+
+qnn_status qnn_activation_table(qnn_activation kind, qnn_dtype x_dtype, qnn_qparams x_q, qnn_dtype y_dtype,
+                                qnn_qparams y_q, uint8_t *table)
+{
+    if (!table)
+        return fail(QNN_ERR_NULL, "activation_table: table is NULL");
+    if (kind < QNN_ACT_GELU || kind > QNN_ACT_HARD_SWISH)
+        return fail(QNN_ERR_QPARAM, "activation_table: unknown activation %d", (int)kind);
+    if ((x_dtype != QNN_UINT8 && x_dtype != QNN_INT8) || (y_dtype != QNN_UINT8 && y_dtype != QNN_INT8))
+        return fail(QNN_ERR_DTYPE, "activation_table: x and y must be uint8 or int8");
+    qnn_status s;
+    if ((s = check_qparams(x_q, "x qparams", 1, x_dtype, false)) != QNN_OK ||
+        (s = check_qparams(y_q, "y qparams", 1, y_dtype, false)) != QNN_OK)
+        return s;
+    Range r;
+    dtype_range(y_dtype, &r);
+    for (int b = 0; b < 256; ++b) {
+        const int q = x_dtype == QNN_INT8 ? (int)(int8_t)b : b;
+        const double x = (double)x_q.scale[0] * (double)(q - x_q.zero_point[0]);
+        double f = 0.0;
+        switch (kind) {
+        case QNN_ACT_GELU: f = 0.5 * x * (1.0 + std::erf(x / std::sqrt(2.0))); break;
+        case QNN_ACT_GELU_TANH:
+            f = 0.5 * x * (1.0 + std::tanh(std::sqrt(2.0 / 3.14159265358979323846) * (x + 0.044715 * x * x * x)));
+            break;
+        case QNN_ACT_SILU: f = x / (1.0 + std::exp(-x)); break;
+        case QNN_ACT_SIGMOID: f = 1.0 / (1.0 + std::exp(-x)); break;
+        case QNN_ACT_TANH: f = std::tanh(x); break;
+        case QNN_ACT_HARD_SWISH: f = x * std::min(std::max(x + 3.0, 0.0), 6.0) / 6.0; break;
+        }
+        // ties away from zero; beyond any code before the integer conversion
+        const double t = std::min(std::max(std::round(f / (double)y_q.scale[0]), -1024.0), 1024.0);
+        table[b] = (uint8_t)std::min(std::max((int64_t)t + y_q.zero_point[0], r.lo), r.hi);
+    }
+    return QNN_OK;
+}
+
+qnn_status qnn_lookup(void *stream, const void *x, const uint8_t *table, int64_t count, void *y)
+{
+    if (count < 0)
+        return fail(QNN_ERR_SHAPE, "lookup: count must be >= 0");
+    if (!table)
+        return fail(QNN_ERR_NULL, "lookup: table is NULL");
+    if (count == 0)
+        return QNN_OK;
+    if (!x || !y)
+        return fail(QNN_ERR_NULL, "lookup: x or y is NULL");
+    LookupArgs a{};
+    a.x = (const uint8_t *)x;
+    a.y = (uint8_t *)y;
+    a.count = count;
+    std::memcpy(a.table, table, 256);
+    const hipError_t e = launch_lookup(a, (hipStream_t)stream);
+    return e == hipSuccess ? QNN_OK : hip_fail(e, "lookup launch");
+}
+
+qnn_status qnn_plan_set_activation(qnn_plan *plan, const uint8_t *table, qnn_dtype y_dtype, qnn_qparams y_q)
+{
+    if (!plan || !table)
+        return fail(QNN_ERR_NULL, "plan_set_activation: plan or table is NULL");
+    if (plan->kind != PLAN_CONV || plan->mode != OUT_REQUANT)
+        return fail(QNN_ERR_UNSUPPORTED, "plan_set_activation: conv and dense plans with 8-bit outputs only");
+    if (plan->fused || plan->acttab)
+        return fail(QNN_ERR_UNSUPPORTED, "plan_set_activation: the plan already has a residual or an activation");
+    if (!plan->conv.linear || (plan->ker.fam != FAM_FLOW && plan->ker.fam != FAM_SMALL))
+        return fail(QNN_ERR_UNSUPPORTED,
+                    "plan_set_activation: matrix products (dense, 1x1 filters without padding) on the short-loop or "
+                    "few-pixel kernels only");
+    if (y_dtype != QNN_UINT8 && y_dtype != QNN_INT8)
+        return fail(QNN_ERR_DTYPE, "plan_set_activation: y must be uint8 or int8");
+    const qnn_status s = check_qparams(y_q, "y qparams", 1, y_dtype, false);
+    if (s != QNN_OK)
+        return s;
+    hipError_t e = hipMalloc((void **)&plan->acttab, 256);
+    if (e != hipSuccess) {
+        plan->acttab = nullptr;
+        return fail(QNN_ERR_ALLOC, "plan_set_activation: table allocation: %s", hipGetErrorString(e));
+    }
+    if ((e = hipMemcpy(plan->acttab, table, 256, hipMemcpyHostToDevice)) != hipSuccess) {
+        (void)hipFree(plan->acttab);
+        plan->acttab = nullptr;
+        return hip_fail(e, "plan_set_activation: table upload");
+    }
+    plan->conv.act = plan->acttab;
+    plan->conv.ydt = y_dtype;
+    plan->y_dt = y_dtype;
+    plan->y_scale = y_q.scale[0];
+    plan->y_zp = y_q.zero_point[0];
+    plan->desc += " +act";
+    return QNN_OK;
 }
 
 qnn_status qnn_plan_set_residual(qnn_plan *plan, qnn_dtype r_dtype, qnn_qparams r_q, int32_t r_ldc, int32_t r_coff,

@@ -274,6 +274,9 @@ struct ConvArgs {
     const uint8_t *res;
     int32_t r_ldc, r_coff, rdt, res_vec;   // res_vec: 16-byte residual rows are 16-byte aligned
     AddArgs fadd;
+    // activation by table: the requantized byte b becomes act[b] (256 bytes in
+    // device memory), before the add; nullptr: none
+    const uint8_t *act;
 };
 
 // Depthwise conv arguments (channel multiplier 1).
@@ -308,6 +311,14 @@ struct DwArgs {
     int32_t lrs, loff0, lcols, lbytes, bthreads;
     int32_t seg;            // strips of dw3_pixels() output pixels per work item: 1, 2 or 4
     int32_t items;          // work items: N * Ho * ceil(Wo / (dw3_pixels() * seg)) * C / 8 (< 2^31)
+};
+
+// Elementwise y = table[x] of bytes; the table travels with the arguments.
+struct LookupArgs {
+    const uint8_t *x;
+    uint8_t *y;
+    int64_t count;
+    uint32_t table[64];
 };
 
 // Elementwise requantize / add arguments.
@@ -434,7 +445,7 @@ bool flow_short(int tile);
 int flow_groups(int tile);
 int flow_wave_tile(int tile);   // channels x pixels of one wave
 size_t flow_lds_bytes(int tile, int nk, bool linear);   // LDS of a launch (fused-add tables included)
-hipError_t launch_conv_flow(const ConvArgs &a, int tile, hipStream_t st);
+hipError_t launch_conv_flow(const ConvArgs &a, int tile, hipStream_t st);   // a.act: linear plans only
 // Kernel for few output pixels (conv_small.hip): channels x pixels per
 // workgroup, the reduction split over its eight waves.
 enum SmallTile {
@@ -541,6 +552,7 @@ hipError_t launch_requantize(const ReqArgs &a, int xdt, int ydt, bool aligned, h
 hipError_t launch_cache_sweep(const void *buf, size_t bytes, int *sink, hipStream_t st);
 hipError_t launch_flip_bytes(const uint8_t *in, uint8_t *out, size_t n, hipStream_t st);
 hipError_t launch_add(const AddArgs &a, int adt, int bdt, int ydt, bool aligned, hipStream_t st);
+hipError_t launch_lookup(const LookupArgs &a, hipStream_t st);
 // Builds AddArgs::tab (512 int32) for operand dtypes adt and bdt (0 uint8, 1 int8).
 hipError_t launch_add_table(const AddArgs &a, int adt, int bdt, int32_t *tab, hipStream_t st);
 

@@ -43,7 +43,7 @@ EXPORTS = [
     "qnn_conv2d_plan_create", "qnn_depthwise_conv2d_plan_create", "qnn_dense_plan_create",
     "qnn_conv2d_plan_create_wt", "qnn_depthwise_conv2d_plan_create_wt", "qnn_dense_plan_create_wt",
     "qnn_requantize_plan_create", "qnn_plan_run", "qnn_plan_run_timed", "qnn_time_next_kernel", "qnn_plan_run_noalloc",
-    "qnn_plan_set_residual", "qnn_plan_run_residual", "qnn_plan_workspace_size",
+    "qnn_plan_set_residual", "qnn_plan_run_residual", "qnn_plan_set_activation", "qnn_activation_table", "qnn_lookup", "qnn_plan_workspace_size",
     "qnn_plan_describe", "qnn_set_tuning_file", "qnn_plan_destroy",
 ]
 
@@ -160,6 +160,12 @@ def lib() -> ctypes.CDLL:
     L.qnn_plan_run_noalloc.restype = st
     L.qnn_plan_set_residual.argtypes = [P, st, QParams, i32, i32, st, QParams, Clamp, st]
     L.qnn_plan_set_residual.restype = st
+    L.qnn_plan_set_activation.argtypes = [P, P, st, QParams]
+    L.qnn_plan_set_activation.restype = st
+    L.qnn_activation_table.argtypes = [st, st, QParams, st, QParams, P]
+    L.qnn_activation_table.restype = st
+    L.qnn_lookup.argtypes = [P, P, P, i64, P]
+    L.qnn_lookup.restype = st
     L.qnn_plan_run_residual.argtypes = [P, P, P, P, P, P]
     L.qnn_plan_run_residual.restype = st
     L.qnn_plan_workspace_size.argtypes = [P]
@@ -299,7 +305,7 @@ def abi_version() -> int:
 class Plan:
     """A prepared conv / depthwise / dense / requantize (owns device memory)."""
 
-    def __init__(self, handle: ctypes.c_void_p, in_shape, in_dtype, out_shape, out_dtype, y_ldc_shape=None):
+    def __init__(self, handle: ctypes.c_void_p, in_shape, in_dtype, out_shape, out_dtype, y_ldc_shape=None, out_q=None):
         self._h = handle
         self.in_shape = tuple(in_shape)
         self.in_dtype = in_dtype
@@ -307,6 +313,7 @@ class Plan:
         self.out_dtype = out_dtype
         self.y_ldc_shape = tuple(y_ldc_shape or out_shape)
         self.residual = None   # (shape, dtype) of a fused add's residual
+        self.out_q = out_q     # (scale, zp) of an 8-bit output
 
     @property
     def handle(self):
@@ -324,15 +331,34 @@ class Plan:
         """qnn_plan_set_residual: the plan then stores qnn.add(its conv
         output, a residual of the output's pixels) with the output qparams
         o_*; run it with run(x, out, workspace, residual=r), r of shape
-        (N, Ho, Wo, r_ldc) (r_ldc defaults to the output channels)."""
-        N, Ho, Wo, K = self.out_shape
+        (N, Ho, Wo, r_ldc), dense: (M, r_ldc) (r_ldc defaults to the output channels)."""
+        *pixels, K = self.out_shape
         r_ldc = K if r_ldc is None else r_ldc
         rdt, odt = _NAME_DT[r_dtype], _NAME_DT[o_dtype]
         rq, oq = _Q(r_scale, r_zp, 1), _Q(o_scale, o_zp, 1)
         _check(lib().qnn_plan_set_residual(self._h, rdt, rq.q, r_ldc, r_coff, odt, oq.q, _clamp(act),
                                            _ROUND[rounding]))
         self.out_dtype = _DT_TORCH[odt]
-        self.residual = ((N, Ho, Wo, r_ldc), _DT_TORCH[rdt])
+        self.residual = ((*pixels, r_ldc), _DT_TORCH[rdt])
+        return self
+
+    def set_activation(self, kind, y_scale, y_zp, y_dtype="i8"):
+        """qnn_plan_set_activation: the plan then stores the activation of its
+        output, with the qparams y_*; kind is one of ACTIVATIONS, or a table of
+        256 bytes (numpy uint8, by the output's byte).  A set_residual may
+        follow."""
+        if isinstance(kind, str):
+            if self.out_q is None:
+                raise ValueError("an activation needs a plan with 8-bit outputs")
+            scale, zp = self.out_q
+            table = activation_table(kind, {v: k for k, v in _NAME_DT.items()}[_TORCH_DT[self.out_dtype]], scale, zp,
+                                     y_dtype, y_scale, y_zp)
+        else:
+            table = _byte_table(kind)
+        yq = _Q(y_scale, y_zp, 1)
+        _check(lib().qnn_plan_set_activation(self._h, table.ctypes.data_as(ctypes.c_void_p), _NAME_DT[y_dtype], yq.q))
+        self.out_dtype = _DT_TORCH[_NAME_DT[y_dtype]]
+        self.out_q = (y_scale, y_zp)
         return self
 
     def new_output(self, device="cuda"):
@@ -433,7 +459,7 @@ def conv2d_plan(x_shape, x_dtype, x_scale, x_zp, w: torch.Tensor, w_scale, w_zp,
                                             _ptr(w), K, R, S, wq.q, _ptr(bias), cp, _NAME_DT[y_dtype], yq.q,
                                             _clamp(act), _ROUND[rounding], y_ldc, y_coff))
     return Plan(h, x_shape, _DT_TORCH[_NAME_DT[x_dtype]], (N, Ho, Wo, K), _DT_TORCH[_NAME_DT[y_dtype]],
-                (N, Ho, Wo, y_ldc))
+                (N, Ho, Wo, y_ldc), None if y_dtype == "i32" else (y_scale, y_zp))
 
 
 def depthwise_conv2d_plan(x_shape, x_dtype, x_scale, x_zp, w: torch.Tensor, w_scale, w_zp, bias=None,
@@ -480,7 +506,8 @@ def dense_plan(M, K, x_dtype, x_scale, x_zp, w: torch.Tensor, w_scale, w_zp, bia
         _check(lib().qnn_dense_plan_create(ctypes.byref(h), _stream(stream), _NAME_DT[x_dtype], M, K, xq.q, _ptr(w),
                                            Nd, wq.q, _ptr(bias), _NAME_DT[y_dtype], yq.q, _clamp(act),
                                            _ROUND[rounding], y_ldc))
-    return Plan(h, (M, K), _DT_TORCH[_NAME_DT[x_dtype]], (M, Nd), _DT_TORCH[_NAME_DT[y_dtype]], (M, y_ldc))
+    return Plan(h, (M, K), _DT_TORCH[_NAME_DT[x_dtype]], (M, Nd), _DT_TORCH[_NAME_DT[y_dtype]], (M, y_ldc),
+                None if y_dtype == "i32" else (y_scale, y_zp))
 
 
 def requantize_plan(shape, x_dtype, x_scale, x_zp, y_scale, y_zp, y_dtype="u8", act=None,
@@ -589,6 +616,44 @@ def add(a: torch.Tensor, a_scale, a_zp, b: torch.Tensor, b_scale, b_zp, y_scale,
     aq, bq, yq = _Q(a_scale, a_zp, 1), _Q(b_scale, b_zp, 1), _Q(y_scale, y_zp, 1)
     _check(lib().qnn_add(_stream(stream), _ptr(a), _dt(a), aq.q, _ptr(b), _dt(b), bq.q, a.numel(), _ptr(out), ydt,
                          yq.q, _clamp(act), _ROUND[rounding]))
+    return out
+
+
+# Activations by name (qnn_activation).
+ACTIVATIONS = {"gelu": 0, "gelu_tanh": 1, "silu": 2, "sigmoid": 3, "tanh": 4, "hard_swish": 5}
+
+
+def _byte_table(table) -> np.ndarray:
+    t = np.ascontiguousarray(table)
+    if t.dtype not in (np.uint8, np.int8) or t.shape != (256,):
+        raise ValueError("a table is 256 bytes (uint8 or int8)")
+    return t.view(np.uint8)
+
+
+def activation_table(kind: str, x_dtype, x_scale, x_zp, y_dtype, y_scale, y_zp) -> np.ndarray:
+    """qnn_activation_table: the 256 output bytes (uint8), by the input's byte."""
+    table = np.zeros(256, np.uint8)
+    xq, yq = _Q(x_scale, x_zp, 1), _Q(y_scale, y_zp, 1)
+    _check(lib().qnn_activation_table(ACTIVATIONS[kind], _NAME_DT[x_dtype], xq.q, _NAME_DT[y_dtype], yq.q,
+                                      table.ctypes.data_as(ctypes.c_void_p)))
+    return table
+
+
+def lookup(x: torch.Tensor, table, y_dtype="i8", out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """y = table[x] by bytes (x u8 or i8, `table` 256 bytes on the host): an
+    activation where a plan has none in its epilogue."""
+    _contig(x, "x")
+    if x.dtype not in (torch.uint8, torch.int8):
+        raise TypeError(f"lookup takes u8 or i8, not {x.dtype}")
+    ydt = _NAME_DT[y_dtype]
+    if ydt == INT32:
+        raise TypeError("lookup gives u8 or i8")
+    if out is None:
+        out = torch.empty(x.shape, dtype=_DT_TORCH[ydt], device=x.device)
+    _contig(out, "out")
+    _check_out(out, tuple(x.shape), ydt, whole=True)
+    _check(lib().qnn_lookup(_stream(stream), _ptr(x), _byte_table(table).ctypes.data_as(ctypes.c_void_p), x.numel(),
+                            _ptr(out)))
     return out
 
 
