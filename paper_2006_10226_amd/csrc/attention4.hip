@@ -26,7 +26,8 @@
 // output is linear in the weights, so any u gives the same quotient.
 //
 // The four waves of a workgroup take every fourth 32 tokens and are joined
-// through LDS.
+// through LDS. Where few rows meet a long cache, its tokens are split over
+// workgroups, whose sums (unscaled, with their offsets) a second kernel joins.
 #include "cache4.h"
 
 #include <algorithm>
@@ -51,6 +52,12 @@ struct AttnArgs {
     int32_t tokens, requests, q_heads, group;   // group: query heads of a cache head
     int32_t width, max_q, causal, window;
     int32_t tiles;          // row tiles of a request and cache head
+    // a long cache in parts of `chunk` tokens, each a workgroup's: their sums
+    // [part][query row][DP] and (offset, sum p) [part][query row], row = token *
+    // q_heads + head, which a second kernel joins (parts == 1: neither)
+    int32_t parts, chunk;
+    float *part_o;
+    float2 *part_p;
     int32_t total;          // workgroups with work, at most
     float scale;            // scale * log2(e), times the query's own scale
     int32_t q_zp;
@@ -76,6 +83,30 @@ __device__ __forceinline__ Span seen(const AttnArgs &a, int ctx, int nq, int que
     s.hi = a.causal ? min(held, p1 + 1) : held;
     s.lo = a.window > 0 && p0 >= a.window ? p0 - a.window + 1 : 0;
     return s;
+}
+
+// The part of a span that workgroup `part` takes: whole steps of 32 tokens, the
+// last part to the end whatever the host took for the longest.
+__device__ __forceinline__ Span part_of(const AttnArgs &a, Span s, int part)
+{
+    const int64_t from = (s.lo & ~31) + (int64_t)part * a.chunk;
+    if (part < a.parts - 1)
+        s.hi = (int)min((int64_t)s.hi, from + a.chunk);
+    if (part > 0)
+        s.lo = (int)min(from, (int64_t)INT32_MAX);
+    return s;
+}
+
+// A request's first query row, and its number of queries.
+__device__ __forceinline__ int queries(const AttnArgs &a, int b, int *nq)
+{
+    if (!a.cu) {
+        *nq = 1;
+        return b;
+    }
+    const int first = min(max(a.cu[b], 0), a.tokens);
+    *nq = min(max(min(a.cu[b + 1], a.tokens) - first, 0), a.max_q);
+    return first;
 }
 
 // max over the four lanes that hold a row's tokens
@@ -169,14 +200,18 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
         return;
     const int tile = a.tiles - 1 - work % a.tiles;
     work /= a.tiles;
+    const int part = work % a.parts;
+    work /= a.parts;
     const int kvh = work % a.c.heads, b = work / a.c.heads;
-    const int first = a.cu ? min(max(a.cu[b], 0), a.tokens) : b;
-    const int nq = a.cu ? min(max(min(a.cu[b + 1], a.tokens) - first, 0), a.max_q) : 1;
+    int nq;
+    const int first = queries(a, b, &nq);
     const int rows = nq * a.group, row0 = tile * 16 * R;
     if (row0 >= rows)
         return;
     const int ctx = max(a.ctx[b], 0);
-    const Span span = seen(a, ctx, nq, row0 / a.group, (min(row0 + 16 * R, rows) - 1) / a.group);
+    const Span span = part_of(a, seen(a, ctx, nq, row0 / a.group, (min(row0 + 16 * R, rows) - 1) / a.group), part);
+    if (part > 0 && span.lo >= span.hi)
+        return;
 
     // ---- queries, as the second operand: lane (n, g) holds channels 8 (g KS +
     // k) .. + 7 of row n for step k
@@ -442,6 +477,20 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
         if (row >= rows)
             continue;
         const int i = row / a.group, h = row - i * a.group;
+        if (a.parts > 1) {
+            const size_t at = (size_t)part * a.tokens * a.q_heads + (size_t)(first + i) * a.q_heads +
+                              (kvh * a.group + h);
+            float *const p = a.part_o + at * DP;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < NV; j += 4)
+                    *(f4 *)(p + (g * 4 + e) * NV + j) =
+                        f4{acc[r][j][e], acc[r][j + 1][e], acc[r][j + 2][e], acc[r][j + 3][e]};
+            if (g == 0)
+                a.part_p[at] = float2{off[r], total[r]};
+            continue;
+        }
         const int64_t at = (int64_t)(first + i) * a.o_ld + (int64_t)(kvh * a.group + h) * a.c.dim;
         const float inv = total[r] == 0.0f ? 0.0f : 1.0f / total[r];
 #pragma unroll
@@ -469,8 +518,79 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
     }
 }
 
-// Row blocks of 16 that a wave holds.
-int row_blocks(const qnn_attention_params &p, int group) { return (int64_t)p.max_q * group <= 16 ? 1 : 2; }
+// Joins the parts of every query row: DP / 4 lanes a row, four channels each.
+template <int DP>
+__global__ void __launch_bounds__(256) join_kernel(AttnArgs a, int blocks)
+{
+    constexpr int kLanes = DP / 4;
+    const int lane = threadIdx.x % kLanes;
+    const int64_t at = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;   // (request, query, head)
+    const int head = (int)(at % a.q_heads);
+    const int64_t bi = at / a.q_heads;
+    const int b = (int)(bi / a.max_q), i = (int)(bi % a.max_q);
+    if (b >= a.requests)
+        return;
+    int nq;
+    const int first = queries(a, b, &nq);
+    if (i >= nq)
+        return;
+    // the parts that its tile's workgroups wrote
+    const int row0 = (i * a.group + head % a.group) / (16 * blocks) * (16 * blocks);
+    const Span span = seen(a, max(a.ctx[b], 0), nq, row0 / a.group,
+                           (min(row0 + 16 * blocks, nq * a.group) - 1) / a.group);
+    const int parts = span.lo < span.hi ? (int)min((int64_t)a.parts, ((int64_t)span.hi - (span.lo & ~31) + a.chunk - 1) / a.chunk) : 1;
+    const size_t row = (size_t)(first + i) * a.q_heads + head, rows = (size_t)a.tokens * a.q_heads;
+    float most = kNone;
+    for (int s = 0; s < parts; ++s)
+        most = fmaxf(most, a.part_p[s * rows + row].x);
+    f4 o = f4{0, 0, 0, 0};
+    float total = 0.0f;
+    for (int s = 0; s < parts; ++s) {
+        const float2 p = a.part_p[s * rows + row];
+        const float down = __builtin_amdgcn_exp2f(p.x - most);
+        o += *(const f4 *)(a.part_o + (s * rows + row) * DP + lane * 4) * down;
+        total += p.y * down;
+    }
+    if (lane * 4 >= a.c.dim)
+        return;
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    store_out(a, (int64_t)(first + i) * a.o_ld + (int64_t)head * a.c.dim + lane * 4, v);
+}
+
+struct Shape {
+    int blocks;
+    int64_t tiles;
+    int parts, chunk;
+};
+
+// Grid of a call: parts of the cache where the row tiles alone would leave the
+// device idle, of at least a step (128 tokens) each.
+Shape shape_of(const qnn_attention_params &p, int group, int heads, int page_size, bool packed)
+{
+    Shape s;
+    const int64_t max_q = packed ? p.max_q : 1;
+    s.blocks = max_q * group <= 16 ? 1 : 2;
+    s.tiles = (max_q * group + 16 * s.blocks - 1) / (16 * s.blocks);
+    int64_t span = (int64_t)p.table_width * page_size;
+    if (p.max_ctx > 0)
+        span = std::min<int64_t>(span, p.max_ctx);
+    if (p.window > 0)
+        span = std::min<int64_t>(span, (int64_t)p.window + (16 * s.blocks + group - 1) / group + 32);
+    const int64_t base = s.tiles * heads * std::max(p.requests, 1);
+    const int64_t want = 8 * (int64_t)device_cus();
+    int64_t parts = std::min<int64_t>((want + base - 1) / base, (span + 127) / 128);
+    parts = base >= want ? 1 : std::max<int64_t>(1, std::min<int64_t>(parts, 128));
+    const int64_t chunk = ((span + parts - 1) / parts + 127) / 128 * 128;
+    s.parts = (int)std::max<int64_t>(1, (span + chunk - 1) / chunk);
+    s.chunk = (int)std::min<int64_t>(chunk, 1 << 30);
+    return s;
+}
+
+size_t parts_bytes(const Shape &s, const qnn_attention_params &p, int dp)
+{
+    return s.parts == 1 ? 0 : (size_t)s.parts * p.tokens * p.q_heads * (dp * sizeof(float) + sizeof(float2));
+}
 
 template <int DP>
 hipError_t launch_attention(const AttnArgs &a, int blocks, hipStream_t st)
@@ -480,6 +600,10 @@ hipError_t launch_attention(const AttnArgs &a, int blocks, hipStream_t st)
         launch_main((attention4_kernel<DP, 1>), grid, block, 0, st, a);
     else
         launch_main((attention4_kernel<DP, 2>), grid, block, 0, st, a);
+    if (a.parts > 1) {
+        const int64_t rows = (int64_t)a.requests * a.max_q * a.q_heads;
+        join_kernel<DP><<<dim3((unsigned)((rows + 1024 / DP - 1) / (1024 / DP))), dim3(256), 0, st>>>(a, blocks);
+    }
     return hipGetLastError();
 }
 
@@ -492,9 +616,14 @@ extern "C" {
 
 size_t qnn_attention4_workspace_size(qnn_cache4 cache, qnn_attention_params p)
 {
-    (void)cache;
-    (void)p;
-    return 0;
+    // sizes that qnn_attention4 refuses need none
+    if (qnn_cache4_page_bytes(cache.page_size, cache.heads, cache.head_dim) == 0 || p.q_heads < cache.heads ||
+        p.q_heads % cache.heads || p.tokens <= 0 || p.requests <= 0 || p.max_q < 1 || p.table_width < 1)
+        return 0;
+    // the same for calls with cu_q and without (one query each): the larger
+    const int group = p.q_heads / cache.heads, dp = cache4_padded(cache.head_dim);
+    return std::max(parts_bytes(shape_of(p, group, cache.heads, cache.page_size, true), p, dp),
+                    parts_bytes(shape_of(p, group, cache.heads, cache.page_size, false), p, dp));
 }
 
 qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qparams q_q, qnn_cache4 cache,
@@ -537,7 +666,6 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
         return fail(QNN_ERR_UNSUPPORTED, "attention4: rows of q and o must be aligned to 8 elements");
     if (qnn_attention4_workspace_size(cache, p) > workspace_bytes)
         return fail(QNN_ERR_SHAPE, "attention4: the workspace is smaller than qnn_attention4_workspace_size()");
-    (void)workspace;
     a.q = q;
     a.o = o;
     a.table = table;
@@ -566,14 +694,25 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
         a.o_lo = (int32_t)r.lo;
         a.o_hi = (int32_t)r.hi;
     }
-    const int blocks = row_blocks(p, a.group);
-    const int64_t tiles = ((int64_t)a.max_q * a.group + 16 * blocks - 1) / (16 * blocks);
-    const int64_t total = tiles * a.c.heads * p.requests;
-    if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || total >= (int64_t(1) << 31) - 8)
+    const Shape g = shape_of(p, a.group, a.c.heads, cache.page_size, cu_q != nullptr);
+    const int64_t total = g.tiles * g.parts * a.c.heads * p.requests;
+    if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || total >= (int64_t(1) << 31) - 8 ||
+        (int64_t)p.requests * a.max_q * p.q_heads >= (int64_t(1) << 31))
         return fail(QNN_ERR_UNSUPPORTED, "attention4: too many row tiles");
-    a.tiles = (int32_t)tiles;
+    a.tiles = (int32_t)g.tiles;
     a.total = (int32_t)total;
+    a.parts = g.parts;
+    a.chunk = g.chunk;
+    const int blocks = g.blocks;
     const int dp = cache4_padded(a.c.dim);
+    if (a.parts > 1) {
+        if (!workspace)
+            return fail(QNN_ERR_NULL, "attention4: the call needs a workspace");
+        if ((uintptr_t)workspace & 15)
+            return fail(QNN_ERR_UNSUPPORTED, "attention4: the workspace must be 16-byte aligned");
+        a.part_o = (float *)workspace;
+        a.part_p = (float2 *)(a.part_o + (size_t)a.parts * a.tokens * a.q_heads * dp);
+    }
     const hipStream_t st = (hipStream_t)stream;
     const hipError_t e = dp == 64    ? launch_attention<64>(a, blocks, st)
                          : dp == 128 ? launch_attention<128>(a, blocks, st)
