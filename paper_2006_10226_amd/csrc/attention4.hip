@@ -121,21 +121,20 @@ __device__ __forceinline__ float row_sum(float v)
     return v + __shfl_xor(v, 32);
 }
 
-// Eight query values of element type dt at p.
-__device__ __forceinline__ void load_q8(const uint8_t *p, int dt, int zp, float (&x)[8])
+// Eight query values of element type dt from their bytes (8-bit ones in the
+// first two words).
+__device__ __forceinline__ void unpack_q8(u4 w, int dt, int zp, float (&x)[8])
 {
     if (dt == QNN_FLOAT16) {
-        const h8 h = *(const h8 *)p;
+        const h8 h = __builtin_bit_cast(h8, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             x[i] = (float)h[i];
     } else if (dt == QNN_BFLOAT16) {
-        const u4 w = *(const u4 *)p;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             x[i] = __builtin_bit_cast(float, i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
     } else {
-        const u2 w = *(const u2 *)p;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t b = (w[i >> 2] >> (8 * (i & 3))) & 0xffu;
@@ -191,56 +190,147 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
 
-    // XCD x takes the x-th eighth of the list: the row tiles of one cache head
-    // follow each other there, the longest (causal) first
-    const int share = (a.total + 7) >> 3;
-    const int xcd = blockIdx.x & 7;
-    int work = xcd * share + (blockIdx.x >> 3);
-    if (work >= min(a.total, (xcd + 1) * share))
-        return;
-    const int tile = a.tiles - 1 - work % a.tiles;
-    work /= a.tiles;
-    const int part = work % a.parts;
-    work /= a.parts;
-    const int kvh = work % a.c.heads, b = work / a.c.heads;
+    int tile = 0, part, kvh, b;
+    if (a.tiles == 1) {
+        // nothing is shared: the first parts of every request, then the second ones
+        // (of the longer requests only), ..., dealt to the XCDs in turn
+        kvh = blockIdx.x % a.c.heads;
+        const int rest = blockIdx.x / a.c.heads;
+        b = rest % a.requests;
+        part = rest / a.requests;
+        if (part >= a.parts)
+            return;
+    } else {
+        // XCD x takes the x-th eighth of the list: the row tiles of one cache head
+        // follow each other there, the longest (causal) first
+        const int share = (a.total + 7) >> 3;
+        const int xcd = blockIdx.x & 7;
+        int work = xcd * share + (blockIdx.x >> 3);
+        if (work >= min(a.total, (xcd + 1) * share))
+            return;
+        tile = a.tiles - 1 - work % a.tiles;
+        work /= a.tiles;
+        part = work % a.parts;
+        work /= a.parts;
+        kvh = work % a.c.heads;
+        b = work / a.c.heads;
+    }
+    const int ctx = max(a.ctx[b], 0);
     int nq;
     const int first = queries(a, b, &nq);
     const int rows = nq * a.group, row0 = tile * 16 * R;
     if (row0 >= rows)
         return;
-    const int ctx = max(a.ctx[b], 0);
     const Span span = part_of(a, seen(a, ctx, nq, row0 / a.group, (min(row0 + 16 * R, rows) - 1) / a.group), part);
     if (part > 0 && span.lo >= span.hi)
         return;
 
     // ---- queries, as the second operand: lane (n, g) holds channels 8 (g KS +
-    // k) .. + 7 of row n for step k
-    u4 q[R][KS];
-    float qsum[R], fac[R];
+    // k) .. + 7 of row n for step k. Their loads are issued here, in one go, and
+    // used once the first step's are on their way too: a workgroup's few dependent
+    // memory latencies are what a short part costs.
+    u4 raw[R][KS];
     int lo_row[R], hi_row[R];
+    const bool wide = a.q_dt == QNN_FLOAT16 || a.q_dt == QNN_BFLOAT16;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int row = row0 + r * 16 + n;
-        const bool live = row < rows;
-        const int i = live ? row / a.group : 0, h = live ? row - i * a.group : 0;
+        const int row = min(row0 + r * 16 + n, rows - 1);
+        const int i = row / a.group, h = row - i * a.group;
         const Span own = seen(a, ctx, nq, i, i);
         lo_row[r] = own.lo;
         hi_row[r] = own.hi;
-        float x[KS][8], most = 0.0f;
-        const int esize = a.q_dt == QNN_FLOAT16 || a.q_dt == QNN_BFLOAT16 ? 2 : 1;
-        const uint8_t *p = (const uint8_t *)a.q +
-                           ((int64_t)(first + i) * a.q_ld + (int64_t)(kvh * a.group + h) * a.c.dim) * esize;
+        const uint8_t *p = (const uint8_t *)a.q + ((int64_t)(first + i) * a.q_ld + (int64_t)(kvh * a.group + h) * a.c.dim)
+                                                      * (wide ? 2 : 1);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const int ch = 8 * (g * KS + k);
+            const int ch = 8 * (g * KS + k), at = ch < a.c.dim ? ch : 0;
+            if (wide) {
+                raw[r][k] = *(const u4 *)(p + at * 2);
+            } else {
+                const u2 w = *(const u2 *)(p + at);
+                raw[r][k] = u4{w[0], w[1], 0, 0};
+            }
+        }
+    }
+
+    const int P = 1 << a.c.shift;
+    const int32_t *const table = a.table + b * a.table_ld;
+    // What a step reads. Lane (n, g): K of tokens 8 (n / 4) + n % 4 (+ 4), words g
+    // KS on; V and records of tokens 8 g .. + 7, V's unit n. A step is two halves of
+    // 16 tokens, each in one page: their addresses are scalars, which a lane picks
+    // from and adds an offset of its own to.
+    struct Step {
+        uint32_t k[2][KS];
+        u4 v[NW];
+        u4 rk[2], rv[2];
+        bool bad;   // some page is none (uniform), the lane's own
+        bool mine;
+    };
+    struct Pages {
+        int p[2];
+    };
+    const uint32_t off_k = ((n >> 2 & 1) * 8 + (n & 3)) * (DP / 2) + g * KS * 4;
+    const uint32_t off_v = (g & 1) * (4 * DP) + n * NW * 16, off_r = (g & 1) * 32;
+    // pages of the halves (past the last token: the last one's)
+    auto pages = [&](int t0) __attribute__((always_inline)) {
+        return Pages{{table[min(t0, span.hi - 1) >> a.c.shift], table[min(t0 + 16, span.hi - 1) >> a.c.shift]}};
+    };
+    auto fetch = [&](Step &d, int t0, Pages pg) __attribute__((always_inline)) {
+        const uint8_t *half[2];
+        bool ok[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                x[k][e] = 0.0f;
-            if (live && ch < a.c.dim)
-                load_q8(p + ch * esize, a.q_dt, a.q_zp, x[k]);
+        for (int h = 0; h < 2; ++h) {
+            ok[h] = (unsigned)pg.p[h] < (unsigned)a.c.pages;
+            half[h] = a.c.data + (size_t)kvh * a.c.head_bytes + (size_t)(ok[h] ? pg.p[h] : 0) * a.c.page_bytes;
+        }
+        d.bad = !(ok[0] && ok[1]);
+        d.mine = g < 2 ? ok[0] : ok[1];
+        const int in0 = t0 & (P - 1), in1 = (t0 + 16) & (P - 1);   // multiples of 16
+        const uint8_t *const kp = (n < 8 ? half[0] + in0 * (DP / 2) : half[1] + in1 * (DP / 2)) + off_k;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                d.k[s][k] = ((const uint32_t *)(kp + s * 4 * (DP / 2)))[k];
+        const uint8_t *const vp =
+            (g < 2 ? half[0] + (P + in0) * (DP / 2) : half[1] + (P + in1) * (DP / 2)) + off_v;
+#pragma unroll
+        for (int j = 0; j < NW; ++j)
+            d.v[j] = ((const u4 *)vp)[j];
+        const uint8_t *const rp = (g < 2 ? half[0] + P * DP + in0 * 4 : half[1] + P * DP + in1 * 4) + off_r;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            d.rk[j] = ((const u4 *)rp)[j];
+            d.rv[j] = ((const u4 *)(rp + 4 * P))[j];
+        }
+    };
+    // tokens that every row of the tile sees
+    const int all_lo = seen(a, ctx, nq, (min(row0 + 16 * R, rows) - 1) / a.group, (min(row0 + 16 * R, rows) - 1) / a.group).lo;
+    const int all_hi = min(span.hi, seen(a, ctx, nq, row0 / a.group, row0 / a.group).hi);
+    constexpr int kNext = kWaves * 32;
+    int t0 = (span.lo & ~31) + wave * 32;
+    Step d0;
+    Pages pg{{-1, -1}};
+    if (t0 < span.hi) {
+        fetch(d0, t0, pages(t0));
+        pg = pages(t0 + kNext);
+    }
+
+    u4 q[R][KS];
+    float qsum[R], fac[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool live = row0 + r * 16 + n < rows;
+        float x[KS][8], most = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            unpack_q8(raw[r][k], a.q_dt, a.q_zp, x[k]);
+            const bool held = live && 8 * (g * KS + k) < a.c.dim;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[k][e] = held ? x[k][e] : 0.0f;
                 most = fmaxf(most, fabsf(x[k][e]));
+            }
         }
         most = row_max(most);
         // a power of two brings the row's largest to 2^14 .. 2^15: exact for 8-bit
@@ -276,43 +366,8 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
         total[r] = 0.0f;
     }
 
-    const int P = 1 << a.c.shift;
-    const int32_t *const table = a.table + b * a.table_ld;
-    const uint8_t *const data = a.c.data + (size_t)kvh * a.c.head_bytes;
-    // page of token t (a token past the last looks up the last), -1 if the table's entry is none
-    auto page_of = [&](int t) {
-        const int p = table[min(t, span.hi - 1) >> a.c.shift];
-        return (unsigned)p < (unsigned)a.c.pages ? p : -1;
-    };
-    for (int t0 = (span.lo & ~31) + wave * 32; t0 < span.hi; t0 += kWaves * 32) {
-        // lane (n, g): K of tokens 8 (n / 4) + n % 4 (+ 4), words g KS on; V and
-        // records of tokens 8 g .. + 7, V's unit n
-        const int tk = t0 + (n >> 2) * 8, tv = t0 + g * 8;
-        const int pk = page_of(tk), pv = page_of(tv);
-        const uint8_t *const bk = data + (size_t)max(pk, 0) * a.c.page_bytes;
-        const uint8_t *const bv = data + (size_t)max(pv, 0) * a.c.page_bytes;
-        uint32_t kw[2][KS];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const uint32_t *p =
-                (const uint32_t *)(bk + ((tk & (P - 1)) + s * 4 + (n & 3)) * (DP / 2)) + g * KS;
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-                kw[s][k] = p[k];
-        }
-        u4 vw[NW];
-        const u4 *const vp = (const u4 *)(bv + P * (DP / 2) + ((tv & (P - 1)) >> 3) * (4 * DP)) + n * NW;
-#pragma unroll
-        for (int j = 0; j < NW; ++j)
-            vw[j] = vp[j];
-        uint32_t rk[8], rv[8];
-        const uint32_t *const rp = (const uint32_t *)(bv + P * DP) + (tv & (P - 1));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            rk[j] = rp[j];
-            rv[j] = rp[P + j];
-        }
-
+    auto step = [&](const Step &d, int t0) __attribute__((always_inline)) {
+        const int tv = t0 + g * 8;
         // ---- scores: sc[r][j] of token tv + j
         f4 sc[R][2];
 #pragma unroll
@@ -322,7 +377,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
                 sc[r][s] = f4{0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const uint32_t w = kw[s][k];
+                const uint32_t w = d.k[s][k];
                 const u4 c = u4{w << 4 & kCode, w & kCode, w >> 4 & kCode, w >> 8 & kCode};
 #pragma unroll
                 for (int r = 0; r < R; ++r)
@@ -333,15 +388,24 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
         float vs[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            // a token that no row sees, or of no page, may hold anything
-            const bool held = tv + j >= span.lo && tv + j < span.hi && pv >= 0;
-            vs[j] = held ? rec_scale(rv[j]) : 0.0f;
-            const float ks = rec_scale(rk[j]), kz = rec_zero(rk[j]);
+            vs[j] = rec_scale(d.rv[j >> 2][j & 3]);
+            const float ks = rec_scale(d.rk[j >> 2][j & 3]), kz = rec_zero(d.rk[j >> 2][j & 3]);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const float x = __builtin_fmaf(-kz, qsum[r], sc[r][j >> 2][j & 3]) * (ks * fac[r]);
-                const bool sees = held && tv + j >= lo_row[r] && tv + j < hi_row[r];
-                sc[r][j >> 2][j & 3] = sees ? x : -INFINITY;
+            for (int r = 0; r < R; ++r)
+                sc[r][j >> 2][j & 3] = __builtin_fmaf(-kz, qsum[r], sc[r][j >> 2][j & 3]) * ks;
+        }
+        if (d.bad || t0 < all_lo || t0 + 32 > all_hi) {
+            // some row doesn't see some token; one that no row sees, or of no page,
+            // may hold anything
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool held = tv + j >= span.lo && tv + j < span.hi && d.mine;
+                vs[j] = held ? vs[j] : 0.0f;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const bool sees = held && tv + j >= lo_row[r] && tv + j < hi_row[r];
+                    sc[r][j >> 2][j & 3] = sees ? sc[r][j >> 2][j & 3] : -INFINITY;
+                }
             }
         }
         u4 pw[R];
@@ -353,7 +417,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
                 top = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    p[j] = __builtin_amdgcn_exp2f(sc[r][j >> 2][j & 3] - off[r]);
+                    p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r][j >> 2][j & 3], fac[r], -off[r]));
                     w[j] = p[j] * vs[j];
                     sum += p[j];
                     top = fmaxf(top, w[j]);
@@ -366,7 +430,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
                 float most = kNone;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float x = sc[r][j >> 2][j & 3];
+                    const float x = sc[r][j >> 2][j & 3] * fac[r];
                     most = fmaxf(most, fmaxf(x + __builtin_amdgcn_logf(vs[j]), x - 90.0f));
                 }
                 most = fmaxf(row_max(most), off[r]);
@@ -394,7 +458,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
                 u4 c;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    c[e] = (i == 0 ? vw[v][e] << 4 : vw[v][e] >> (4 * i - 4)) & kCode;
+                    c[e] = (i == 0 ? d.v[v][e] << 4 : d.v[v][e] >> (4 * i - 4)) & kCode;
 #pragma unroll
                 for (int r = 0; r < R; ++r)
                     acc[r][v * 4 + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
@@ -405,11 +469,46 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
         u4 z;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            z[e] = __builtin_amdgcn_perm(rv[2 * e + 1], rv[2 * e], 0x0c040c00u) << 4;   // low bytes
+            z[e] = __builtin_amdgcn_perm(d.rv[e >> 1][2 * (e & 1) + 1], d.rv[e >> 1][2 * (e & 1)], 0x0c040c00u) << 4;   // low bytes
 #pragma unroll
         for (int r = 0; r < R; ++r)
             zacc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, z), __builtin_bit_cast(h8, pw[r]),
                                                              zacc[r], 0, 0, 0);
+    };
+    if (R == 1 && t0 < span.hi) {
+        // two steps in registers: one is fetched, its pages' numbers a step earlier
+        // still, while the other is computed
+        Step d1;
+        while (true) {
+            const bool second = t0 + kNext < span.hi;
+            if (second) {
+                fetch(d1, t0 + kNext, pg);
+                pg = pages(t0 + 2 * kNext);
+            }
+            step(d0, t0);
+            if (!second)
+                break;
+            t0 += kNext;
+            const bool third = t0 + kNext < span.hi;
+            if (third) {
+                fetch(d0, t0 + kNext, pg);
+                pg = pages(t0 + 2 * kNext);
+            }
+            step(d1, t0);
+            if (!third)
+                break;
+            t0 += kNext;
+        }
+    }
+    if (R > 1 && t0 < span.hi) {
+        while (true) {
+            step(d0, t0);
+            t0 += kNext;
+            if (t0 >= span.hi)
+                break;
+            fetch(d0, t0, pg);
+            pg = pages(t0 + kNext);
+        }
     }
 
     // ---- the waves' parts joined: common offset, sums through LDS
@@ -518,40 +617,63 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
     }
 }
 
-// Joins the parts of every query row: DP / 4 lanes a row, four channels each.
+// Joins the parts of every query row: DP / 4 lanes hold its channels, and `crews`
+// (a power of two, up to 1024 / DP) of such lanes share the parts, whose sums meet
+// in LDS: with one crew, 64 parts were 128 dependent memory latencies.
 template <int DP>
-__global__ void __launch_bounds__(256) join_kernel(AttnArgs a, int blocks)
+__global__ void __launch_bounds__(256) join_kernel(AttnArgs a, int blocks, int crews)
 {
     constexpr int kLanes = DP / 4;
-    const int lane = threadIdx.x % kLanes;
-    const int64_t at = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;   // (request, query, head)
+    __shared__ f4 sums[256];
+    __shared__ float sum_p[256 / kLanes];
+    const int lane = threadIdx.x % kLanes, crew = threadIdx.x / kLanes % crews;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / (kLanes * crews);   // (request, query, head)
     const int head = (int)(at % a.q_heads);
     const int64_t bi = at / a.q_heads;
     const int b = (int)(bi / a.max_q), i = (int)(bi % a.max_q);
-    if (b >= a.requests)
-        return;
-    int nq;
-    const int first = queries(a, b, &nq);
-    if (i >= nq)
-        return;
-    // the parts that its tile's workgroups wrote
-    const int row0 = (i * a.group + head % a.group) / (16 * blocks) * (16 * blocks);
-    const Span span = seen(a, max(a.ctx[b], 0), nq, row0 / a.group,
-                           (min(row0 + 16 * blocks, nq * a.group) - 1) / a.group);
-    const int parts = span.lo < span.hi ? (int)min((int64_t)a.parts, ((int64_t)span.hi - (span.lo & ~31) + a.chunk - 1) / a.chunk) : 1;
+    int nq = 0, first = 0;
+    if (b < a.requests)
+        first = queries(a, b, &nq);
+    const bool live = i < nq;
     const size_t row = (size_t)(first + i) * a.q_heads + head, rows = (size_t)a.tokens * a.q_heads;
-    float most = kNone;
-    for (int s = 0; s < parts; ++s)
-        most = fmaxf(most, a.part_p[s * rows + row].x);
     f4 o = f4{0, 0, 0, 0};
-    float total = 0.0f;
-    for (int s = 0; s < parts; ++s) {
+    float total = 0.0f, most = kNone;
+    int parts = 0;
+    if (live) {
+        // the parts that its tile's workgroups wrote
+        const int row0 = (i * a.group + head % a.group) / (16 * blocks) * (16 * blocks);
+        const Span span = seen(a, max(a.ctx[b], 0), nq, row0 / a.group,
+                               (min(row0 + 16 * blocks, nq * a.group) - 1) / a.group);
+        parts = span.lo < span.hi
+                    ? (int)min((int64_t)a.parts, ((int64_t)span.hi - (span.lo & ~31) + a.chunk - 1) / a.chunk)
+                    : 1;
+        // the offset of all parts, each lane looking at some (the row's lanes are in one
+        // wave, or fill several that look at the same ones)
+        for (int s = lane; s < parts; s += kLanes)
+            most = fmaxf(most, a.part_p[s * rows + row].x);
+    }
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1)
+        most = fmaxf(most, __shfl_xor(most, d));
+#pragma unroll 4
+    for (int s = crew; s < parts; s += crews) {
         const float2 p = a.part_p[s * rows + row];
         const float down = __builtin_amdgcn_exp2f(p.x - most);
         o += *(const f4 *)(a.part_o + (s * rows + row) * DP + lane * 4) * down;
         total += p.y * down;
     }
-    if (lane * 4 >= a.c.dim)
+    if (crews > 1) {
+        sums[threadIdx.x] = o;
+        if (lane == 0)
+            sum_p[threadIdx.x / kLanes] = total;
+        __syncthreads();
+        if (crew == 0)
+            for (int c = 1; c < crews; ++c) {
+                o += sums[threadIdx.x + c * kLanes];
+                total += sum_p[threadIdx.x / kLanes + c];
+            }
+    }
+    if (!live || crew != 0 || lane * 4 >= a.c.dim)
         return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
@@ -601,8 +723,11 @@ hipError_t launch_attention(const AttnArgs &a, int blocks, hipStream_t st)
     else
         launch_main((attention4_kernel<DP, 2>), grid, block, 0, st, a);
     if (a.parts > 1) {
-        const int64_t rows = (int64_t)a.requests * a.max_q * a.q_heads;
-        join_kernel<DP><<<dim3((unsigned)((rows + 1024 / DP - 1) / (1024 / DP))), dim3(256), 0, st>>>(a, blocks);
+        int crews = 1;
+        while (crews < 1024 / DP && crews * 4 < a.parts)
+            crews *= 2;
+        const int64_t rows = (int64_t)a.requests * a.max_q * a.q_heads, per = 1024 / DP / crews;
+        join_kernel<DP><<<dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st>>>(a, blocks, crews);
     }
     return hipGetLastError();
 }
