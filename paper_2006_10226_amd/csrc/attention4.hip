@@ -58,7 +58,8 @@ struct AttnArgs {
     int32_t parts, chunk;
     float *part_o;
     float2 *part_p;
-    int32_t total;          // workgroups with work, at most
+    int32_t stripes, unit_tiles;   // shares of a head's row tiles, and the tiles of one (tiles > 1)
+    int32_t grid;
     float scale;            // scale * log2(e), times the query's own scale
     int32_t q_zp;
     float o_scale;
@@ -182,7 +183,7 @@ __device__ __forceinline__ void store_out(const AttnArgs &a, int64_t at, const f
 }
 
 template <int DP, int R>
-__global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
+__global__ void __launch_bounds__(kWaves * 64, DP == 256 && R == 2 ? 1 : 2) attention4_kernel(AttnArgs a)
 {
     constexpr int KS = DP / 32;    // K-steps of a score; words of K of a lane and token
     constexpr int NV = DP / 16;    // 16-channel blocks of the output
@@ -201,19 +202,17 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
         if (part >= a.parts)
             return;
     } else {
-        // XCD x takes the x-th eighth of the list: the row tiles of one cache head
-        // follow each other there, the longest (causal) first
-        const int share = (a.total + 7) >> 3;
-        const int xcd = blockIdx.x & 7;
-        int work = xcd * share + (blockIdx.x >> 3);
-        if (work >= min(a.total, (xcd + 1) * share))
+        // row tiles of one cache head read the same tokens: they follow each other on
+        // one XCD, or, where the heads don't fill the XCDs evenly, are dealt to
+        // `stripes` of them; the longest (causal) first
+        const int unit = (int)(blockIdx.x & 7) + 8 * (int)(blockIdx.x / (8u * a.unit_tiles * a.parts));
+        const int rest = (int)(blockIdx.x / 8u % ((unsigned)a.unit_tiles * a.parts));
+        tile = unit % a.stripes + a.stripes * (a.unit_tiles - 1 - rest / a.parts);
+        part = rest % a.parts;
+        kvh = unit / a.stripes % a.c.heads;
+        b = unit / a.stripes / a.c.heads;
+        if (tile >= a.tiles || b >= a.requests)
             return;
-        tile = a.tiles - 1 - work % a.tiles;
-        work /= a.tiles;
-        part = work % a.parts;
-        work /= a.parts;
-        kvh = work % a.c.heads;
-        b = work / a.c.heads;
     }
     const int ctx = max(a.ctx[b], 0);
     int nq;
@@ -475,7 +474,8 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
             zacc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, z), __builtin_bit_cast(h8, pw[r]),
                                                              zacc[r], 0, 0, 0);
     };
-    if (R == 1 && t0 < span.hi) {
+    constexpr bool kTwo = R == 1 || DP <= 128;   // registers for two steps
+    if (kTwo && t0 < span.hi) {
         // two steps in registers: one is fetched, its pages' numbers a step earlier
         // still, while the other is computed
         Step d1;
@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attention4_kernel(AttnArgs a)
             t0 += kNext;
         }
     }
-    if (R > 1 && t0 < span.hi) {
+    if (!kTwo && t0 < span.hi) {
         while (true) {
             step(d0, t0);
             t0 += kNext;
@@ -680,6 +680,11 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a, int blocks, int c
     store_out(a, (int64_t)(first + i) * a.o_ld + (int64_t)head * a.c.dim + lane * 4, v);
 }
 
+// Least tokens of a part: below, the join's launch and latencies cost more than
+// the walk they save (one request of 1000 tokens 14.0 us in 8 parts, 11.6 us in
+// one; 48 of a window of 1024 24.5 and 21.7 us).
+constexpr int kLeastPart = 768;
+
 struct Shape {
     int blocks;
     int64_t tiles;
@@ -687,7 +692,7 @@ struct Shape {
 };
 
 // Grid of a call: parts of the cache where the row tiles alone would leave the
-// device idle, of at least a step (128 tokens) each.
+// device idle.
 Shape shape_of(const qnn_attention_params &p, int group, int heads, int page_size, bool packed)
 {
     Shape s;
@@ -701,7 +706,7 @@ Shape shape_of(const qnn_attention_params &p, int group, int heads, int page_siz
         span = std::min<int64_t>(span, (int64_t)p.window + (16 * s.blocks + group - 1) / group + 32);
     const int64_t base = s.tiles * heads * std::max(p.requests, 1);
     const int64_t want = 8 * (int64_t)device_cus();
-    int64_t parts = std::min<int64_t>((want + base - 1) / base, (span + 127) / 128);
+    int64_t parts = std::min<int64_t>((want + base - 1) / base, span / kLeastPart);
     parts = base >= want ? 1 : std::max<int64_t>(1, std::min<int64_t>(parts, 128));
     const int64_t chunk = ((span + parts - 1) / parts + 127) / 128 * 128;
     s.parts = (int)std::max<int64_t>(1, (span + chunk - 1) / chunk);
@@ -717,7 +722,7 @@ size_t parts_bytes(const Shape &s, const qnn_attention_params &p, int dp)
 template <int DP>
 hipError_t launch_attention(const AttnArgs &a, int blocks, hipStream_t st)
 {
-    const dim3 grid((unsigned)((a.total + 7) / 8 * 8)), block(kWaves * 64);
+    const dim3 grid((unsigned)a.grid), block(kWaves * 64);
     if (blocks == 1)
         launch_main((attention4_kernel<DP, 1>), grid, block, 0, st, a);
     else
@@ -820,12 +825,17 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
         a.o_hi = (int32_t)r.hi;
     }
     const Shape g = shape_of(p, a.group, a.c.heads, cache.page_size, cu_q != nullptr);
-    const int64_t total = g.tiles * g.parts * a.c.heads * p.requests;
-    if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || total >= (int64_t(1) << 31) - 8 ||
+    // heads of requests, dealt to eight XCDs
+    const int64_t heads = (int64_t)a.c.heads * p.requests;
+    a.stripes = g.tiles == 1 ? 1 : heads % 8 == 0 ? 1 : heads % 4 == 0 ? 2 : heads % 2 == 0 ? 4 : 8;
+    const int64_t unit_tiles = (g.tiles + a.stripes - 1) / a.stripes;
+    const int64_t grid = g.tiles == 1 ? heads * g.parts : (heads * a.stripes + 7) / 8 * 8 * unit_tiles * g.parts;
+    if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || grid >= (int64_t(1) << 31) ||
         (int64_t)p.requests * a.max_q * p.q_heads >= (int64_t(1) << 31))
         return fail(QNN_ERR_UNSUPPORTED, "attention4: too many row tiles");
     a.tiles = (int32_t)g.tiles;
-    a.total = (int32_t)total;
+    a.unit_tiles = (int32_t)unit_tiles;
+    a.grid = (int32_t)grid;
     a.parts = g.parts;
     a.chunk = g.chunk;
     const int blocks = g.blocks;

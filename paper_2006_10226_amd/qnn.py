@@ -694,44 +694,57 @@ _FLOAT_NAME = {"u8": torch.uint8, "i8": torch.int8, "f16": torch.float16, "bf16"
 _NO_Q = QParams(None, None, 0)
 
 
-def _here(device: torch.device, **tensors):
-    """Every given tensor on `device`, which must be the current one."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {device}, the current device is cuda:{torch.cuda.current_device()}"
-                         if device.type == "cuda" else "the tensors must be device tensors")
+def _one_q(scale, zp) -> QParams:
+    """Per-tensor qparams of two numbers (a tenth of _Q's time, which small calls see)."""
+    return QParams(ctypes.pointer(ctypes.c_float(scale)), ctypes.pointer(ctypes.c_int32(zp)), 1)
+
+
+def _here(index: int, **tensors):
+    """Every given tensor on device `index`, which must be the current one."""
+    if index < 0:
+        raise ValueError("the tensors must be device tensors")
+    if index != torch.cuda.current_device():
+        raise ValueError(f"tensors on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
     for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"{name} is on {t.device}, not on cuda:{index}")
 
 
 def _ints(t: Optional[torch.Tensor], name: str, count: Optional[int] = None):
     """A contiguous int32 vector (of `count` entries)."""
     if t is None:
         return
-    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (count is not None and t.numel() != count):
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (count is not None and len(t) != count):
         raise ValueError(f"{name} must be a contiguous int32 vector" + ("" if count is None else f" of {count} entries")
                          + f", not {tuple(t.shape)} {t.dtype}")
 
 
 def _heads(t: torch.Tensor, name: str, shape) -> int:
     """Row stride of a [tokens][heads][head_dim] tensor whose rows are contiguous."""
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
-    T, H, D = t.shape
-    if D > 1 and t.stride(2) != 1 or H > 1 and t.stride(1) != D:
+    T, H, D = shape
+    row, head, one = t.stride()
+    if D > 1 and one != 1 or H > 1 and head != D:
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    if T > 1 and t.stride(0) < H * D:
-        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)})")
-    return t.stride(0) if T > 1 else max(H * D, t.stride(0))
+    if T <= 1:
+        return max(H * D, row)
+    if row < H * D:
+        raise ValueError(f"{name}: rows overlap (stride {row})")
+    return row
 
 
 def _table(t: torch.Tensor, rows: int) -> int:
     if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"the block table must be int32 [{rows}][pages] with contiguous rows, not {tuple(t.shape)} "
                          f"{t.dtype}")
-    if rows > 1 and t.stride(0) < t.shape[1]:
-        raise ValueError(f"the block table's rows overlap (stride {t.stride(0)})")
-    return t.stride(0) if rows > 1 else t.shape[1]
+    width = t.shape[1]
+    if rows <= 1:
+        return width
+    ld = t.stride(0)
+    if ld < width:
+        raise ValueError(f"the block table's rows overlap (stride {ld})")
+    return ld
 
 
 class Cache4:
@@ -753,7 +766,7 @@ class Cache4:
         if not data.is_cuda:
             raise ValueError("data must be a device tensor")
         self.data, self.num_pages, self.page_size = data, num_pages, page_size
-        self.heads, self.head_dim = heads, head_dim
+        self.heads, self.head_dim, self.device = heads, head_dim, data.get_device()
         self.desc = Cache4Desc(data.data_ptr(), num_pages, page_size, heads, head_dim)
 
 
@@ -763,16 +776,15 @@ def cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, slots: torch.
     their scale and zero point) to 4 bits at `slots` (int32; below 0: skipped);
     see qnn_cache4_append.  k and v may be slices of a wider tensor of rows."""
     T = k.shape[0]
-    _here(cache.data.device, k=k, v=v, slots=slots)
+    _here(cache.device, k=k, v=v, slots=slots)
     if k.dtype not in _FLOAT_DT or v.dtype != k.dtype:
         raise TypeError(f"k and v must both be f16, bf16, u8 or i8, not {k.dtype} and {v.dtype}")
     k_ld, v_ld = (_heads(t, n, (T, cache.heads, cache.head_dim)) for t, n in ((k, "k"), (v, "v")))
     _ints(slots, "slots", T)
     whole = k.dtype in (torch.uint8, torch.int8)
-    kq, vq = (_Q(k_scale, k_zp, 1), _Q(v_scale, v_zp, 1)) if whole else (None, None)
     status = lib().qnn_cache4_append(_stream_handle(stream), cache.desc, k.data_ptr(), v.data_ptr(),
-                                     _FLOAT_DT[k.dtype], kq.q if whole else _NO_Q, vq.q if whole else _NO_Q, T, k_ld,
-                                     v_ld, slots.data_ptr())
+                                     _FLOAT_DT[k.dtype], _one_q(k_scale, k_zp) if whole else _NO_Q,
+                                     _one_q(v_scale, v_zp) if whole else _NO_Q, T, k_ld, v_ld, slots.data_ptr())
     if status:
         _check(status)
 
@@ -780,7 +792,7 @@ def cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, slots: torch.
 def cache4_read(cache: Cache4, slots: torch.Tensor, dtype="f16", stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(k, v) at `slots` as [slots][heads][head_dim] of dtype "f16" or "bf16";
     slots outside the cache give zeros.  See qnn_cache4_read."""
-    _here(cache.data.device, slots=slots)
+    _here(cache.device, slots=slots)
     _ints(slots, "slots")
     T = slots.numel()
     dt = _FLOAT_NAME[dtype]
@@ -810,8 +822,8 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
     if q.dim() != 3:
         raise ValueError("q must be [tokens][heads][head_dim]")
     T, Hq, D = q.shape
-    B = ctx.numel()
-    _here(cache.data.device, q=q, block_table=block_table, ctx=ctx, cu_q=cu_q, out=out, workspace=workspace)
+    B = len(ctx)
+    _here(cache.device, q=q, block_table=block_table, ctx=ctx, cu_q=cu_q, out=out, workspace=workspace)
     if q.dtype not in _FLOAT_DT:
         raise TypeError(f"q must be f16, bf16, u8 or i8, not {q.dtype}")
     _ints(ctx, "ctx")
@@ -822,9 +834,9 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
         out = torch.empty((T, Hq, D), dtype=odt, device=q.device)
     if out.dtype != odt:
         raise ValueError(f"out is {out.dtype}, not {odt}")
-    p = AttentionParams(T, Hq, B, block_table.shape[1] if block_table.dim() == 2 else 0, q_ld,
-                        _heads(out, "out", (T, Hq, D)), _table(block_table, B), max_q, max_ctx, int(bool(causal)),
-                        window, D ** -0.5 if scale is None else scale)
+    table_ld = _table(block_table, B)
+    p = AttentionParams(T, Hq, B, block_table.shape[1], q_ld, _heads(out, "out", (T, Hq, D)), table_ld, max_q, max_ctx,
+                        1 if causal else 0, window, D ** -0.5 if scale is None else scale)
     need = lib().qnn_attention4_workspace_size(cache.desc, p)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
@@ -833,12 +845,12 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
         have = workspace.numel() * workspace.element_size()
-    qq = _Q(q_scale, q_zp, 1) if q.dtype in (torch.uint8, torch.int8) else None
-    oq = _Q(y_scale, y_zp, 1) if odt in (torch.uint8, torch.int8) else None
-    status = lib().qnn_attention4(_stream_handle(stream), q.data_ptr(), _FLOAT_DT[q.dtype], qq.q if qq else _NO_Q,
-                                  cache.desc, block_table.data_ptr(), ctx.data_ptr(),
-                                  None if cu_q is None else cu_q.data_ptr(), p, out.data_ptr(), _FLOAT_DT[odt],
-                                  oq.q if oq else _NO_Q, None if workspace is None else workspace.data_ptr(), have)
+    qq = _one_q(q_scale, q_zp) if q.dtype in (torch.uint8, torch.int8) else _NO_Q
+    oq = _one_q(y_scale, y_zp) if odt in (torch.uint8, torch.int8) else _NO_Q
+    status = lib().qnn_attention4(_stream_handle(stream), q.data_ptr(), _FLOAT_DT[q.dtype], qq, cache.desc,
+                                  block_table.data_ptr(), ctx.data_ptr(), None if cu_q is None else cu_q.data_ptr(),
+                                  p, out.data_ptr(), _FLOAT_DT[odt], oq,
+                                  None if workspace is None else workspace.data_ptr(), have)
     if status:
         _check(status)
     return out
@@ -864,7 +876,7 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.
     int32 device tensors."""
     B = lens.numel()
     dev = lens.device
-    _here(dev, new_lens=new_lens, block_table=block_table, free_pages=free_pages, free_count=free_count,
+    _here(lens.get_device(), new_lens=new_lens, block_table=block_table, free_pages=free_pages, free_count=free_count,
           workspace=workspace)
     _ints(lens, "lens")
     _ints(new_lens, "new_lens", B)
