@@ -52,7 +52,7 @@ __device__ __forceinline__ void load8(const void *p, float s, int z, float (&x)[
 }
 
 // Thread -> vector: the workgroup's 256 threads take eight consecutive tokens
-// of one head, K and V (of 2048 / DP passes each), so that the tokens of a V
+// of one head (16 for DP 64, four for 256), K and V, so that the tokens of a V
 // tile are written together.
 template <int DP>
 struct Map {
@@ -61,64 +61,82 @@ struct Map {
     static constexpr int kTokens = kVectors / 2;         // K and V
 };
 
+// V's two-byte units lie 16 bytes apart for one token and side by side for the
+// eight of a tile: they go through LDS, so that neighbouring lanes store
+// neighbouring tokens' (16384 tokens of 8 heads of 128 in f16: APPEND_MEASURED).
 template <int DP, int DT>
 __global__ void __launch_bounds__(256) append_kernel(VecArgs a)
 {
     using M = Map<DP>;
+    __shared__ uint16_t unit[M::kTokens][DP / 4];
     const int lane = threadIdx.x % M::kLanes, vec = threadIdx.x / M::kLanes;
     const bool is_v = vec >= M::kTokens;
     const int head = blockIdx.x % a.c.heads;
-    const int64_t tok = (int64_t)(blockIdx.x / a.c.heads) * M::kTokens + vec % M::kTokens;
-    const int slot = tok < a.tokens ? a.slots[tok] : -1;
-    const int page = slot >> a.c.shift, at = slot & ((1 << a.c.shift) - 1);
-    if (slot < 0 || page >= a.c.pages)
-        return;   // a whole group: the shuffles below stay inside one
-    const int ch = lane * 8;
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (ch < a.c.dim) {
-        const int64_t off = tok * (is_v ? a.v_ld : a.k_ld) + head * a.c.dim + ch;
-        constexpr int size = DT == QNN_UINT8 || DT == QNN_INT8 ? 1 : 2;
-        load8<DT>((const uint8_t *)(is_v ? a.v : a.k) + off * size, is_v ? a.vs : a.ks, is_v ? a.vz : a.kz, x);
-    }
-    constexpr float kMost = 0x1p126f;
-    float lo = 0.0f, hi = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -kMost), kMost) : 0.0f;
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-    }
-#pragma unroll
-    for (int d = 1; d < M::kLanes; d <<= 1) {
-        lo = fminf(lo, __shfl_xor(lo, d));
-        hi = fmaxf(hi, __shfl_xor(hi, d));
-    }
-    // the scale keeps 16 significant bits, rounded up so that 15 steps span the range
-    const uint32_t sb = (__builtin_bit_cast(uint32_t, (hi - lo) / 15.0f) + 0xffu) & 0xffffff00u;
-    const float s = __builtin_bit_cast(float, sb);
-    const float div = sb ? s : 1.0f;
-    const float z = fminf(__builtin_rintf(-lo / div), 15.0f);
-    uint32_t c[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        c[i] = (uint32_t)fminf(fmaxf(__builtin_rintf(x[i] / div) + z, 0.0f), 15.0f);
-    uint8_t *base = a.c.data + (size_t)page * a.c.page_bytes + (size_t)head * a.c.head_bytes;
+    const int64_t tok0 = (int64_t)(blockIdx.x / a.c.heads) * M::kTokens, tok = tok0 + vec % M::kTokens;
     const int P = 1 << a.c.shift;
-    if (!is_v) {
-        uint32_t w = 0;
+    // the head's block of a slot's page, nullptr for a slot outside the cache
+    auto block_of = [&](int slot) -> uint8_t * {
+        const int page = slot >> a.c.shift;
+        return slot < 0 || page >= a.c.pages
+                   ? nullptr
+                   : a.c.data + (size_t)page * a.c.page_bytes + (size_t)head * a.c.head_bytes;
+    };
+    // the token whose V unit this thread stores in the end
+    constexpr int kSide = M::kTokens < 8 ? M::kTokens : 8;
+    const int my = threadIdx.x % kSide + threadIdx.x / (kSide * DP / 4) * kSide, my_unit = threadIdx.x / kSide % (DP / 4);
+    const int my_slot = tok0 + my < a.tokens ? a.slots[tok0 + my] : -1;
+    const int slot = tok < a.tokens ? a.slots[tok] : -1;
+    uint8_t *const base = block_of(slot);
+    if (base) {   // a whole group: the shuffles below stay inside one
+        const int at = slot & (P - 1), ch = lane * 8;
+        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (ch < a.c.dim) {
+            const int64_t off = tok * (is_v ? a.v_ld : a.k_ld) + head * a.c.dim + ch;
+            constexpr int size = DT == QNN_UINT8 || DT == QNN_INT8 ? 1 : 2;
+            load8<DT>((const uint8_t *)(is_v ? a.v : a.k) + off * size, is_v ? a.vs : a.ks, is_v ? a.vz : a.kz, x);
+        }
+        constexpr float kMost = 0x1p126f;
+        float lo = 0.0f, hi = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w |= c[2 * i] << (4 * i) | c[2 * i + 1] << (16 + 4 * i);
-        *(uint32_t *)(base + at * (DP / 2) + lane * 4) = w;
-    } else {
-        uint8_t *tile = base + P * (DP / 2) + (at >> 3) * (4 * DP) + (at & 7) * 2;
+        for (int i = 0; i < 8; ++i) {
+            x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -kMost), kMost) : 0.0f;
+            lo = fminf(lo, x[i]);
+            hi = fmaxf(hi, x[i]);
+        }
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-            *(uint16_t *)(tile + (lane * 2 + u) * 16) =
-                (uint16_t)(c[4 * u] | c[4 * u + 1] << 4 | c[4 * u + 2] << 8 | c[4 * u + 3] << 12);
+        for (int d = 1; d < M::kLanes; d <<= 1) {
+            lo = fminf(lo, __shfl_xor(lo, d));
+            hi = fmaxf(hi, __shfl_xor(hi, d));
+        }
+        // the scale keeps 16 significant bits, rounded up so that 15 steps span the range
+        const uint32_t sb = (__builtin_bit_cast(uint32_t, (hi - lo) / 15.0f) + 0xffu) & 0xffffff00u;
+        const float s = __builtin_bit_cast(float, sb);
+        const float div = sb ? s : 1.0f;
+        const float z = fminf(__builtin_rintf(-lo / div), 15.0f);
+        uint32_t c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            c[i] = (uint32_t)fminf(fmaxf(__builtin_rintf(x[i] / div) + z, 0.0f), 15.0f);
+        if (!is_v) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w |= c[2 * i] << (4 * i) | c[2 * i + 1] << (16 + 4 * i);
+            *(uint32_t *)(base + at * (DP / 2) + lane * 4) = w;
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                unit[vec - M::kTokens][lane * 2 + u] =
+                    (uint16_t)(c[4 * u] | c[4 * u + 1] << 4 | c[4 * u + 2] << 8 | c[4 * u + 3] << 12);
+        }
+        if (lane == 0)
+            *(uint32_t *)(base + P * DP + (is_v ? 4 * P : 0) + at * 4) = sb | (uint32_t)z;
     }
-    if (lane == 0)
-        *(uint32_t *)(base + P * DP + (is_v ? 4 * P : 0) + at * 4) = sb | (uint32_t)z;
+    __syncthreads();
+    if (uint8_t *const mine = block_of(my_slot)) {
+        const int at = my_slot & (P - 1);
+        *(uint16_t *)(mine + P * (DP / 2) + (at >> 3) * (4 * DP) + my_unit * 16 + (at & 7) * 2) = unit[my][my_unit];
+    }
 }
 
 template <int DP, int DT>

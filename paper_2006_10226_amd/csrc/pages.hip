@@ -15,6 +15,7 @@
 namespace qnn {
 namespace {
 
+struct Head;
 struct PagesArgs {
     int32_t requests, shift;   // page size 1 << shift
     int32_t *lens;
@@ -30,17 +31,24 @@ struct PagesArgs {
     int32_t *status;
     // workspace: head, the old lengths, the running counts of pages given
     // back and taken (requests + 1 each)
-    int32_t *head, *old, *gone, *got;
+    Head *head;
+    int32_t *old, *gone, *got;
 };
-enum { HEAD_GO = 0, HEAD_COUNT = 1, HEAD_GONE = 2, HEAD_INTS = 4 };
 
 constexpr int kSumThreads = 1024;
 
 // Pages of n tokens.
 __device__ __forceinline__ int pages_of(int n, int shift) { return (int)(((int64_t)n + (1 << shift) - 1) >> shift); }
 
+// What the sums say: whether anything is done, the stack's count with the pages
+// given back on it, those, and the new tokens.
+struct Head {
+    int go, count, gone, tokens;
+};
+
 // Largest i with at[i] <= v, at[0 .. n] ascending with at[0] <= v < at[n].
-__device__ __forceinline__ int find(const int32_t *at, int n, int v)
+template <typename A>
+__device__ __forceinline__ int find(const A &at, int n, int v)
 {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
@@ -53,19 +61,22 @@ __device__ __forceinline__ int find(const int32_t *at, int n, int v)
     return lo;
 }
 
+// T: int where no sum of a call can pass 32 bits, else long long.
+template <typename T>
 struct Sums {
-    long long gone, got, add;
+    T gone, got, add;
 };
 
 // Running sums over the workgroup's threads, exclusive, and their totals.
-__device__ __forceinline__ Sums block_scan(Sums v, Sums *total)
+template <typename T>
+__device__ __forceinline__ Sums<T> block_scan(Sums<T> v, Sums<T> *total)
 {
-    __shared__ Sums wave_sum[kSumThreads / 64];
+    __shared__ Sums<T> wave_sum[kSumThreads / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Sums s = v;
+    Sums<T> s = v;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const long long a = __shfl_up(s.gone, d), b = __shfl_up(s.got, d), c = __shfl_up(s.add, d);
+        const T a = __shfl_up(s.gone, d), b = __shfl_up(s.got, d), c = __shfl_up(s.add, d);
         if (lane >= d) {
             s.gone += a;
             s.got += b;
@@ -76,10 +87,10 @@ __device__ __forceinline__ Sums block_scan(Sums v, Sums *total)
     if (lane == 63)
         wave_sum[wave] = s;
     __syncthreads();
-    Sums before{0, 0, 0}, all{0, 0, 0};
-#pragma unroll
+    Sums<T> before{0, 0, 0}, all{0, 0, 0};
+#pragma unroll 4
     for (int w = 0; w < kSumThreads / 64; ++w) {
-        const Sums t = wave_sum[w];
+        const Sums<T> t = wave_sum[w];
         if (w < wave) {
             before.gone += t.gone;
             before.got += t.got;
@@ -90,34 +101,40 @@ __device__ __forceinline__ Sums block_scan(Sums v, Sums *total)
         all.add += t.add;
     }
     *total = all;
-    return Sums{before.gone + s.gone - v.gone, before.got + s.got - v.got, before.add + s.add - v.add};
+    return Sums<T>{before.gone + s.gone - v.gone, before.got + s.got - v.got, before.add + s.add - v.add};
 }
 
-// One workgroup of kSumThreads: the running sums, the decision, the lengths.
-__device__ void sum_requests(const PagesArgs &a)
+// One workgroup of kSumThreads: the running sums (to the workspace and cu, and to
+// `lists` where all requests fit it), the decision, the lengths.
+struct Lists {
+    int old[kSumThreads], now[kSumThreads], gone[kSumThreads], got[kSumThreads], cu[kSumThreads + 1];
+};
+template <typename T, bool LISTS>
+__device__ __forceinline__ Head sum_requests(const PagesArgs &a, Lists *lists)
 {
     const int tid = threadIdx.x;
+    const int n = *a.free_count;
     const long long most = (long long)a.width << a.shift;
-    long long gone = 0, got = 0, add = 0;
-    int bad = 0;
+    T gone = 0, got = 0, add = 0;
+    int bad = n < 0 || n > a.capacity, old = 0, now = 0;
+    Sums<T> s{0, 0, 0};
     for (int at = 0; at < a.requests; at += kSumThreads) {
         const int b = at + tid;
-        Sums v{0, 0, 0};
-        int old = 0;
+        Sums<T> v{0, 0, 0};
         if (b < a.requests) {
             old = a.lens[b];
-            const int now = a.new_lens[b];
+            now = a.new_lens[b];
             if (old < 0 || now < 0 || old > most || now > most) {
                 bad = 1;
             } else {
                 const int have = pages_of(old, a.shift), want = pages_of(now, a.shift);
-                v = Sums{max(have - want, 0), max(want - have, 0), max(now - old, 0)};
+                v = Sums<T>{max(have - want, 0), max(want - have, 0), max(now - old, 0)};
             }
         }
-        Sums total;
-        const Sums s = block_scan(v, &total);
-        // a sum beyond 32 bits is refused below, by its 64-bit total
-        if (b < a.requests) {
+        Sums<T> total;
+        s = block_scan<T>(v, &total);
+        if (!LISTS && b < a.requests) {
+            // a sum beyond 32 bits is refused below, by its total
             a.old[b] = old;
             a.gone[b] = (int)(gone + s.gone);
             a.got[b] = (int)(got + s.got);
@@ -127,66 +144,81 @@ __device__ void sum_requests(const PagesArgs &a)
         got += total.got;
         add += total.add;
     }
-    const int n = *a.free_count;
-    bad = __syncthreads_or(bad) || n < 0 || n > a.capacity;
+    bad = __syncthreads_or(bad);
     int status = 0;
     if (bad)
         status = -1;
     else if (add > a.tokens)
         status = -2;
-    else if (n + gone > a.capacity)
+    else if (n + (long long)gone > a.capacity)
         status = -3;
-    else if (got > n + gone)
-        status = (int)min(got - n - gone, (long long)INT32_MAX);
-    for (int b = tid; b < a.requests; b += kSumThreads) {
-        if (status)
-            a.cu[b] = 0;
-        else
-            a.lens[b] = a.new_lens[b];
+    else if (got > n + (long long)gone)
+        status = (int)min((long long)got - n - gone, (long long)INT32_MAX);
+    if constexpr (LISTS) {
+        if (tid < a.requests) {
+            lists->old[tid] = old;
+            lists->now[tid] = now;
+            lists->gone[tid] = s.gone;
+            lists->got[tid] = s.got;
+            lists->cu[tid] = s.add;
+            a.cu[tid] = status ? 0 : s.add;
+            if (!status)
+                a.lens[tid] = now;
+        }
+    } else {
+        for (int b = tid; b < a.requests; b += kSumThreads) {
+            if (status)
+                a.cu[b] = 0;
+            else
+                a.lens[b] = a.new_lens[b];
+        }
     }
+    const Head h{status == 0, (int)(n + (long long)gone), status ? 0 : (int)gone, status ? 0 : (int)add};
     if (tid == 0) {
-        a.gone[a.requests] = (int)gone;
-        a.got[a.requests] = (int)got;
-        a.cu[a.requests] = status ? 0 : (int)add;
-        a.head[HEAD_GO] = status == 0;
-        a.head[HEAD_COUNT] = (int)(n + gone);
-        a.head[HEAD_GONE] = status ? 0 : (int)gone;
+        a.cu[a.requests] = h.tokens;
         *a.status = status;
         if (status == 0)
-            *a.free_count = (int)(n + gone - got);
+            *a.free_count = (int)(n + (long long)gone - got);
+        if constexpr (LISTS) {
+            lists->cu[a.requests] = h.tokens;
+        } else {
+            a.gone[a.requests] = (int)gone;
+            *a.head = h;
+        }
     }
+    return h;
 }
 
 // Pages given back: element `at` on, by `stride`.
-__device__ __forceinline__ void give_back(const PagesArgs &a, int at, int stride)
+template <typename G, typename N>
+__device__ __forceinline__ void give_back(const PagesArgs &a, const Head &h, const G &gone, const N &now, int at,
+                                          int stride)
 {
-    const int n = a.head[HEAD_GONE], count = a.head[HEAD_COUNT];
-    for (int i = at; i < n; i += stride) {
-        const int b = find(a.gone, a.requests, i);
-        // the lengths have been updated: lens[b] is the new one
-        int32_t *entry = a.table + b * a.ld + pages_of(a.lens[b], a.shift) + (i - a.gone[b]);
-        a.free_pages[count - 1 - i] = *entry;
+    for (int i = at; i < h.gone; i += stride) {
+        const int b = find(gone, a.requests, i);
+        int32_t *entry = a.table + b * a.ld + pages_of(now[b], a.shift) + (i - gone[b]);
+        a.free_pages[h.count - 1 - i] = *entry;
         *entry = -1;
     }
 }
 
 // Slots, positions and new table entries: tokens `at` on, by `stride`.
-__device__ __forceinline__ void place_tokens(const PagesArgs &a, int at, int stride)
+template <typename C, typename O, typename G>
+__device__ __forceinline__ void place_tokens(const PagesArgs &a, const Head &h, const C &cu, const O &olds, const G &got,
+                                             int at, int stride)
 {
-    const int go = a.head[HEAD_GO], count = a.head[HEAD_COUNT];
-    const int total = go ? a.cu[a.requests] : 0;
     for (int t = at; t < a.tokens; t += stride) {
         int slot = -1, pos = 0;
-        if (t < total) {
-            const int b = find(a.cu, a.requests, t);
-            const int old = a.old[b];
-            pos = old + t - a.cu[b];
+        if (t < h.tokens) {
+            const int b = find(cu, a.requests, t);
+            const int old = olds[b];
+            pos = old + t - cu[b];
             const int j = pos >> a.shift, have = pages_of(old, a.shift), off = pos & ((1 << a.shift) - 1);
             int page;
             if (j < have) {
                 page = a.table[b * a.ld + j];
             } else {
-                page = a.free_pages[count - 1 - (a.got[b] + j - have)];
+                page = a.free_pages[h.count - 1 - (got[b] + j - have)];
                 if (off == 0)   // a new page's first token is a new one
                     a.table[b * a.ld + j] = page;
             }
@@ -198,16 +230,29 @@ __device__ __forceinline__ void place_tokens(const PagesArgs &a, int at, int str
     }
 }
 
-__global__ void __launch_bounds__(kSumThreads) sum_kernel(PagesArgs a) { sum_requests(a); }
+// Everything in one workgroup, the running sums in LDS: few requests and tokens.
+template <typename T>
+__global__ void __launch_bounds__(kSumThreads) resize_kernel(PagesArgs a)
+{
+    __shared__ Lists lists;
+    const Head h = sum_requests<T, true>(a, &lists);
+    __syncthreads();
+    give_back(a, h, lists.gone, lists.now, threadIdx.x, kSumThreads);
+    __syncthreads();   // the pages taken may be among those given back
+    place_tokens(a, h, lists.cu, lists.old, lists.got, threadIdx.x, kSumThreads);
+}
+
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(PagesArgs a) { sum_requests<long long, false>(a, nullptr); }
 
 __global__ void __launch_bounds__(256) give_back_kernel(PagesArgs a)
 {
-    give_back(a, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+    // (the lengths have been updated: lens holds the new ones)
+    give_back(a, *a.head, a.gone, a.lens, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 __global__ void __launch_bounds__(256) place_kernel(PagesArgs a)
 {
-    place_tokens(a, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+    place_tokens(a, *a.head, a.cu, a.old, a.got, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 size_t round16(size_t v) { return (v + 15) / 16 * 16; }
@@ -223,7 +268,7 @@ size_t qnn_pages_workspace_size(int32_t requests)
 {
     if (requests < 0)
         return 0;
-    return HEAD_INTS * sizeof(int32_t) + 3 * round16(((size_t)requests + 1) * sizeof(int32_t));
+    return sizeof(Head) + 3 * round16(((size_t)requests + 1) * sizeof(int32_t));
 }
 
 qnn_status qnn_pages_resize(void *stream, int32_t requests, int32_t page_size, int32_t *lens, const int32_t *new_lens,
@@ -262,11 +307,23 @@ qnn_status qnn_pages_resize(void *stream, int32_t requests, int32_t page_size, i
     a.status = status;
     const size_t row = round16(((size_t)requests + 1) * sizeof(int32_t));
     char *ws = (char *)workspace;
-    a.head = (int32_t *)ws;
-    a.old = (int32_t *)(ws + HEAD_INTS * sizeof(int32_t));
-    a.gone = (int32_t *)(ws + HEAD_INTS * sizeof(int32_t) + row);
-    a.got = (int32_t *)(ws + HEAD_INTS * sizeof(int32_t) + 2 * row);
+    a.head = (Head *)ws;
+    a.old = (int32_t *)(ws + sizeof(Head));
+    a.gone = (int32_t *)(ws + sizeof(Head) + row);
+    a.got = (int32_t *)(ws + sizeof(Head) + 2 * row);
     const hipStream_t st = (hipStream_t)stream;
+    // One launch where a workgroup can do the elements' work in about two passes: a
+    // step of 64 requests 5.0 us, three launches 13; a batch of 1000 with 50000 new
+    // tokens would be 60 passes.
+    if (requests <= kSumThreads && token_capacity <= 2 * kSumThreads) {
+        const int64_t most = (int64_t)requests * table_width * page_size;
+        if (most < (int64_t(1) << 31))
+            launch_main((resize_kernel<int>), dim3(1), dim3(kSumThreads), 0, st, a);
+        else
+            launch_main((resize_kernel<long long>), dim3(1), dim3(kSumThreads), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? QNN_OK : hip_fail(e, "pages_resize launch");
+    }
     launch_main(sum_kernel, dim3(1), dim3(kSumThreads), 0, st, a);
     give_back_kernel<<<256, 256, 0, st>>>(a);
     place_kernel<<<std::max(1, std::min(2048, (int)(((int64_t)token_capacity + 255) / 256))), 256, 0, st>>>(a);

@@ -874,7 +874,7 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.
     request b's new tokens are slots[cu[b]:cu[b + 1]], unused entries -1; status
     (a device int32) is 0, or says why nothing was changed.  All arguments are
     int32 device tensors."""
-    B = lens.numel()
+    B = len(lens)
     dev = lens.device
     _here(lens.get_device(), new_lens=new_lens, block_table=block_table, free_pages=free_pages, free_count=free_count,
           workspace=workspace)
@@ -891,8 +891,7 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.
     if token_capacity < 0:
         raise ValueError("token_capacity must be >= 0")
     out = torch.empty(B + 2 + 2 * token_capacity, dtype=torch.int32, device=dev)
-    cu, status = out[:B + 1], out[B + 1:B + 2]
-    slots, positions = out[B + 2:B + 2 + token_capacity], out[B + 2 + token_capacity:]
+    cu, status, slots, positions = out.split_with_sizes((B + 1, 1, token_capacity, token_capacity))
     code = lib().qnn_pages_resize(_stream_handle(stream), B, page_size, lens.data_ptr(), new_lens.data_ptr(),
                                   block_table.data_ptr(), block_table.shape[1], ld, free_pages.data_ptr(),
                                   free_pages.numel(), free_count.data_ptr(), cu.data_ptr(), slots.data_ptr(),
