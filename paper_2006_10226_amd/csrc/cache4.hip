@@ -51,6 +51,13 @@ __device__ __forceinline__ void load8(const void *p, float s, int z, float (&x)[
     }
 }
 
+// The value of another lane of the same 16 (a DPP control).
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 15, 15, true));
+}
+
 // Thread -> vector: the workgroup's 256 threads take eight consecutive tokens
 // of one head (16 for DP 64, four for 256), K and V, so that the tokens of a V
 // tile are written together.
@@ -63,7 +70,7 @@ struct Map {
 
 // V's two-byte units lie 16 bytes apart for one token and side by side for the
 // eight of a tile: they go through LDS, so that neighbouring lanes store
-// neighbouring tokens' (16384 tokens of 8 heads of 128 in f16: APPEND_MEASURED).
+// neighbouring tokens'.
 template <int DP, int DT>
 __global__ void __launch_bounds__(256) append_kernel(VecArgs a)
 {
@@ -99,24 +106,51 @@ __global__ void __launch_bounds__(256) append_kernel(VecArgs a)
         float lo = 0.0f, hi = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -kMost), kMost) : 0.0f;
+            if constexpr (DT == QNN_FLOAT16 || DT == QNN_BFLOAT16)
+                x[i] = x[i] == x[i] ? __builtin_amdgcn_fmed3f(x[i], -kMost, kMost) : 0.0f;
             lo = fminf(lo, x[i]);
             hi = fmaxf(hi, x[i]);
         }
-#pragma unroll
-        for (int d = 1; d < M::kLanes; d <<= 1) {
-            lo = fminf(lo, __shfl_xor(lo, d));
-            hi = fmaxf(hi, __shfl_xor(hi, d));
+        // over the group: neighbours, pairs, then mirrored eights and sixteens
+        lo = fminf(lo, lane_move<0xb1>(lo));
+        hi = fmaxf(hi, lane_move<0xb1>(hi));
+        lo = fminf(lo, lane_move<0x4e>(lo));
+        hi = fmaxf(hi, lane_move<0x4e>(hi));
+        lo = fminf(lo, lane_move<0x141>(lo));
+        hi = fmaxf(hi, lane_move<0x141>(hi));
+        if constexpr (M::kLanes >= 16) {
+            lo = fminf(lo, lane_move<0x140>(lo));
+            hi = fmaxf(hi, lane_move<0x140>(hi));
+        }
+        if constexpr (M::kLanes >= 32) {
+            lo = fminf(lo, __shfl_xor(lo, 16));
+            hi = fmaxf(hi, __shfl_xor(hi, 16));
         }
         // the scale keeps 16 significant bits, rounded up so that 15 steps span the range
         const uint32_t sb = (__builtin_bit_cast(uint32_t, (hi - lo) / 15.0f) + 0xffu) & 0xffffff00u;
-        const float s = __builtin_bit_cast(float, sb);
-        const float div = sb ? s : 1.0f;
-        const float z = fminf(__builtin_rintf(-lo / div), 15.0f);
+        float s = sb ? __builtin_bit_cast(float, sb) : 1.0f;
+        if (s < 0x1p-100f) {   // the reciprocal below would overflow; exact
+            s *= 0x1p100f;
+            lo *= 0x1p100f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                x[i] *= 0x1p100f;
+        }
+        // x / s by the correctly rounded reciprocal and one step on the remainder,
+        // within 2^-23 of the quotient, and exact where that is a whole number and a
+        // half: 16-bit x and 16 bits of s leave no other quotient within 2^-21 of
+        // one, so the rounding is that of x / s (a full division took three times the
+        // instructions, which bound the kernel)
+        const float inv = 1.0f / s;
+        auto steps = [&](float v) {
+            const float q = v * inv;
+            return __builtin_rintf(__builtin_fmaf(__builtin_fmaf(-q, s, v), inv, q));
+        };
+        const float z = fminf(steps(-lo), 15.0f);
         uint32_t c[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            c[i] = (uint32_t)fminf(fmaxf(__builtin_rintf(x[i] / div) + z, 0.0f), 15.0f);
+            c[i] = (uint32_t)__builtin_amdgcn_fmed3f(steps(x[i]) + z, 0.0f, 15.0f);
         if (!is_v) {
             uint32_t w = 0;
 #pragma unroll
