@@ -238,7 +238,7 @@ __device__ __forceinline__ lds_i32 *fuse_tables()
 // Activation of requantized bytes by table (ConvArgs::act). The 256 bytes are
 // one dword in each of the LDS's 64 banks, so 64 lanes reading any bytes of them
 // never conflict; an element is a read and two or three instructions, whatever
-// the function: dense 8192 x 4096 x 4096 with SiLU and a residual 252 us.
+// the function: dense 8192 x 4096 x 4096 with SiLU and a residual 137 us.
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 
 // LDS home of the table in the instantiations that have an activation.
@@ -430,7 +430,11 @@ __device__ __forceinline__ void store_tile(const ConvArgs &a, v4i (&acc)[TC / WC
     constexpr int NT = WC * WP * 64;
     constexpr int WTC = TC / WC, WTP = TP / WP;
     constexpr int FC = WTC / 16, FP = WTP / 16;
-    static_assert(!FUSE || WTC * WTP <= kFuseMaxWaveTile, "fused add: wave tiles of at most kFuseMaxWaveTile");
+    // Wave tiles beyond kFuseMaxWaveTile leave no registers for the residual while
+    // they hold their accumulators: it is loaded once the tile is staged
+    // (instantiated with an activation only)
+    constexpr bool LATE = FUSE && WTC * WTP > kFuseMaxWaveTile;
+    static_assert(!LATE || ACT, "fused add alone: wave tiles of at most kFuseMaxWaveTile");
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform per wave
@@ -441,8 +445,9 @@ __device__ __forceinline__ void store_tile(const ConvArgs &a, v4i (&acc)[TC / WC
     int32_t tabv[FUSE ? 512 / NT : 1];
     if constexpr (FUSE) {
         static_assert(512 % NT == 0, "the term tables split evenly over the threads");
-        residual_prefetch<TC, TP, NT>(a, c0, p0, rres);
-        if (a.fadd.tab && !a.fadd.flt) {
+        if constexpr (!LATE)
+            residual_prefetch<TC, TP, NT>(a, c0, p0, rres);
+        if (!LATE && a.fadd.tab && !a.fadd.flt) {
 #pragma unroll
             for (int i = 0; i < 512 / NT; ++i)
                 tabv[i] = a.fadd.tab[i * NT + tid];
@@ -515,11 +520,13 @@ __device__ __forceinline__ void store_tile(const ConvArgs &a, v4i (&acc)[TC / WC
         } else {
             requantize(std::integral_constant<Req, Req::CHAN>{});
         }
+        if constexpr (LATE)
+            residual_prefetch<TC, TP, NT>(a, c0, p0, rres);
         if constexpr (FUSE) {
             if (a.fadd.tab && !a.fadd.flt) {
 #pragma unroll
                 for (int i = 0; i < 512 / NT; ++i)
-                    fuse_tables<FUSE>()[i * NT + tid] = tabv[i];
+                    fuse_tables<FUSE>()[i * NT + tid] = LATE ? a.fadd.tab[i * NT + tid] : tabv[i];
             }
         }
         __syncthreads();

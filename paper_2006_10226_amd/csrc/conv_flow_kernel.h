@@ -552,21 +552,17 @@ hipError_t launch_flow_act_from(const ConvArgs &a, int tile, hipStream_t st)
         if (tile != T)
             return launch_flow_act_from<T + 1, FUSE>(a, tile, st);
         constexpr FlowCfg c = kFlowCfg[T];
-        if constexpr (FUSE && !flow_fuse_cfg(T)) {
-            return hipErrorInvalidValue;   // no fused-add instantiation
-        } else {
-            constexpr bool big = c.tc / c.wc * (c.tp / c.wp) >= 128 * 64;   // without term 3 only
-            if (!a.linear || a.mode != OUT_REQUANT || (c.sh && a.nk > c.ns) || (big && (a.asum || a.pcorr)))
-                return hipErrorInvalidValue;
-            const dim3 grid((a.ntiles + 7) / 8 * 8), block(c.wc * c.wp * 64 * c.ks);
-            if (a.flip4)
-                launch_main((conv_flow_kernel<c.tc, c.tp, c.wc, c.wp, c.ns, c.ks, c.sh, false, true, FUSE, true>), grid,
-                            block, 0, st, a);
-            else
-                launch_main((conv_flow_kernel<c.tc, c.tp, c.wc, c.wp, c.ns, c.ks, c.sh, false, false, FUSE, true>), grid,
-                            block, 0, st, a);
-            return hipGetLastError();
-        }
+        constexpr bool big = c.tc / c.wc * (c.tp / c.wp) >= 128 * 64;   // without term 3 only
+        if (!a.linear || a.mode != OUT_REQUANT || (c.sh && a.nk > c.ns) || (big && (a.asum || a.pcorr)))
+            return hipErrorInvalidValue;
+        const dim3 grid((a.ntiles + 7) / 8 * 8), block(c.wc * c.wp * 64 * c.ks);
+        if (a.flip4)
+            launch_main((conv_flow_kernel<c.tc, c.tp, c.wc, c.wp, c.ns, c.ks, c.sh, false, true, FUSE, true>), grid,
+                        block, 0, st, a);
+        else
+            launch_main((conv_flow_kernel<c.tc, c.tp, c.wc, c.wp, c.ns, c.ks, c.sh, false, false, FUSE, true>), grid,
+                        block, 0, st, a);
+        return hipGetLastError();
     } else {
         return hipErrorInvalidValue;
     }

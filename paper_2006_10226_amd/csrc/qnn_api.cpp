@@ -2319,8 +2319,10 @@ qnn_status qnn_plan_set_residual(qnn_plan *plan, qnn_dtype r_dtype, qnn_qparams 
     const ConvArgs &c = plan->conv;
     // the 256 x 256 tile has no fused add: such a plan turns to the fastest
     // tile that has one (fuse_ker), once everything else is in order
-    const ConvKernel ker = plan->ker.fam == FAM_FLOW && !can_fuse(plan->ker) ? plan->fuse_ker : plan->ker;
-    if (plan->mode != OUT_REQUANT || !c.staged || !can_fuse(ker))
+    // (with an activation it has one)
+    const bool any_tile = plan->acttab && plan->ker.fam == FAM_FLOW;
+    const ConvKernel ker = plan->ker.fam == FAM_FLOW && !can_fuse(plan->ker) && !any_tile ? plan->fuse_ker : plan->ker;
+    if (plan->mode != OUT_REQUANT || !c.staged || !(any_tile || can_fuse(ker)))
         return fail(QNN_ERR_UNSUPPORTED,
                     "plan_set_residual: the plan's kernel has no fused-add epilogue (8-bit output staged by the "
                     "tap-walk or LDS-direct kernels whose waves hold at most 64 x 64 outputs)");

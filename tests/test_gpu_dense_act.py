@@ -76,8 +76,6 @@ def test_every_configuration(fam, tile):
         assert d.startswith("conv_dma_flow" if fam == "QNN_FLOW" else "conv_dma_small") and d.endswith(" +act"), d
         log(f"activation {fam}={tile} {c.name}: {d}")
         assert_equal(y, _expect(c, table, yt), f"{fam}={tile} {c.name}: {d}")
-        if fam == "QNN_FLOW" and tile == 6:
-            continue   # the largest tile has no residual add
         # the same with a residual add behind it
         M, N = y.shape
         mid = _expect(c, table, yt)
@@ -156,7 +154,7 @@ def test_add_by_tables_behind_an_activation():
     table = _table(9)
     mid = _expect(c, table, "u8")
     r = np.random.default_rng(0).integers(-128, 128, mid.shape).astype(np.int8)
-    for forced in (dict(QNN_FLOW=0), dict(QNN_SMALL=3)):
+    for forced in (dict(QNN_FLOW=0), dict(QNN_FLOW=6), dict(QNN_SMALL=3)):
         with env(QNN_FLOAT_ADD=0, **forced):
             y, d = _run(c, table, "u8", (r, 0.041, -4, 0.05, 9, "i8"))
         assert d.endswith("+act +add"), d
