@@ -193,7 +193,10 @@ constexpr int wave_target()
     return R == 1 ? (DP == 64 ? 4 : DP == 128 ? 3 : 2) : (DP == 256 ? 1 : 2);
 }
 
-template <int DP, int R>
+// FINE: the weights enter the matrix cores as two f16, their rounding and the
+// rest. 16-bit outputs are rounded as coarsely as one f16; of 8-bit ones about
+// one in 100 would fall on the other side of a step.
+template <int DP, int R, bool FINE>
 __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention4_kernel(AttnArgs a)
 {
     constexpr int KS = DP / 32;    // K-steps of a score; words of K of a lane and token
@@ -420,7 +423,7 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
                 }
             }
         }
-        u4 pw[R];
+        u4 pw[R], pl[FINE ? R : 1];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float p[8], w[8], sum, top;
@@ -459,8 +462,15 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
             h8 h;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                h[j] = (_Float16)w[j];   // rounded to nearest: 2^-12 of each weight at most, in no direction
+                h[j] = (_Float16)w[j];   // rounded to nearest: 2^-11 of each weight at most, in no direction
             pw[r] = __builtin_bit_cast(u4, h);
+            if constexpr (FINE) {
+                h8 l;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    l[j] = (_Float16)(w[j] - (float)h[j]);
+                pl[r] = __builtin_bit_cast(u4, l);
+            }
         }
         // ---- output: V's pieces hold pairs of tokens of four channels
 #pragma unroll
@@ -475,6 +485,12 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
                 for (int r = 0; r < R; ++r)
                     acc[r][v * 4 + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
                         __builtin_bit_cast(h8, c), __builtin_bit_cast(h8, pw[r]), acc[r][v * 4 + i], 0, 0, 0);
+                if constexpr (FINE) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+                        acc[r][v * 4 + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                            __builtin_bit_cast(h8, c), __builtin_bit_cast(h8, pl[r]), acc[r][v * 4 + i], 0, 0, 0);
+                }
             }
         }
         // sum w z by the same cores, every row of the operand z
@@ -483,9 +499,13 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
         for (int e = 0; e < 4; ++e)
             z[e] = __builtin_amdgcn_perm(d.rv[e >> 1][2 * (e & 1) + 1], d.rv[e >> 1][2 * (e & 1)], 0x0c040c00u) << 4;   // low bytes
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r) {
             zacc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, z), __builtin_bit_cast(h8, pw[r]),
                                                              zacc[r], 0, 0, 0);
+            if constexpr (FINE)
+                zacc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                    __builtin_bit_cast(h8, z), __builtin_bit_cast(h8, pl[r]), zacc[r], 0, 0, 0);
+        }
     };
     constexpr bool kTwo = R == 1 || DP <= 128;   // registers for two steps
     if (kTwo && t0 < span.hi) {
@@ -736,10 +756,15 @@ template <int DP>
 hipError_t launch_attention(const AttnArgs &a, int blocks, hipStream_t st)
 {
     const dim3 grid((unsigned)a.grid), block(kWaves * 64);
-    if (blocks == 1)
-        launch_main((attention4_kernel<DP, 1>), grid, block, 0, st, a);
+    const bool fine = a.o_dt == QNN_UINT8 || a.o_dt == QNN_INT8;
+    if (blocks == 1 && fine)
+        launch_main((attention4_kernel<DP, 1, true>), grid, block, 0, st, a);
+    else if (blocks == 1)
+        launch_main((attention4_kernel<DP, 1, false>), grid, block, 0, st, a);
+    else if (fine)
+        launch_main((attention4_kernel<DP, 2, true>), grid, block, 0, st, a);
     else
-        launch_main((attention4_kernel<DP, 2>), grid, block, 0, st, a);
+        launch_main((attention4_kernel<DP, 2, false>), grid, block, 0, st, a);
     if (a.parts > 1) {
         int crews = 1;
         while (crews < 1024 / DP && crews * 4 < a.parts)
