@@ -699,22 +699,25 @@ def _one_q(scale, zp) -> QParams:
     return QParams(ctypes.pointer(ctypes.c_float(scale)), ctypes.pointer(ctypes.c_int32(zp)), 1)
 
 
-def _here(index: int, **tensors):
-    """Every given tensor on device `index`, which must be the current one."""
+def _here(index: int, *tensors):
+    """Every given tensor on device `index`, which must be the current one.
+    (These checks are most of a small call's time on the host: no names or
+    formatting unless something is wrong.)"""
     if index < 0:
         raise ValueError("the tensors must be device tensors")
-    if index != torch.cuda.current_device():
+    if index != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
         raise ValueError(f"tensors on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
-    for name, t in tensors.items():
+    for t in tensors:
         if t is not None and t.get_device() != index:
-            raise ValueError(f"{name} is on {t.device}, not on cuda:{index}")
+            raise ValueError(f"a tensor of {tuple(t.shape)} {t.dtype} is on {t.device}, not on cuda:{index}")
 
 
 def _ints(t: Optional[torch.Tensor], name: str, count: Optional[int] = None):
     """A contiguous int32 vector (of `count` entries)."""
     if t is None:
         return
-    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (count is not None and len(t) != count):
+    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or (count is not None and
+                                                                               t.numel() != count):
         raise ValueError(f"{name} must be a contiguous int32 vector" + ("" if count is None else f" of {count} entries")
                          + f", not {tuple(t.shape)} {t.dtype}")
 
@@ -776,7 +779,7 @@ def cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, slots: torch.
     their scale and zero point) to 4 bits at `slots` (int32; below 0: skipped);
     see qnn_cache4_append.  k and v may be slices of a wider tensor of rows."""
     T = k.shape[0]
-    _here(cache.device, k=k, v=v, slots=slots)
+    _here(cache.device, k, v, slots)
     if k.dtype not in _FLOAT_DT or v.dtype != k.dtype:
         raise TypeError(f"k and v must both be f16, bf16, u8 or i8, not {k.dtype} and {v.dtype}")
     k_ld, v_ld = (_heads(t, n, (T, cache.heads, cache.head_dim)) for t, n in ((k, "k"), (v, "v")))
@@ -792,13 +795,16 @@ def cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, slots: torch.
 def cache4_read(cache: Cache4, slots: torch.Tensor, dtype="f16", stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(k, v) at `slots` as [slots][heads][head_dim] of dtype "f16" or "bf16";
     slots outside the cache give zeros.  See qnn_cache4_read."""
-    _here(cache.device, slots=slots)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return cache4_read(cache, slots, dtype)
+    _here(cache.device, slots)
     _ints(slots, "slots")
     T = slots.numel()
     dt = _FLOAT_NAME[dtype]
-    k, v = torch.empty((2, T, cache.heads, cache.head_dim), dtype=dt, device=cache.data.device).unbind(0)
+    k, v = cache.data.new_empty((2, T, cache.heads, cache.head_dim), dtype=dt).unbind(0)
     ld = cache.heads * cache.head_dim
-    status = lib().qnn_cache4_read(_stream_handle(stream), cache.desc, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(),
+    status = lib().qnn_cache4_read(_stream_handle(), cache.desc, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(),
                                    _FLOAT_DT[dt], ld, ld)
     if status:
         _check(status)
@@ -819,11 +825,15 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
     "i8"; q's by default), 8-bit ones with y_scale and y_zp.  `workspace` is a
     uint8 tensor of attention4_workspace_size() bytes, allocated here if not
     given; two calls that may overlap need one each."""
+    if stream is not None:   # what is allocated here belongs to the stream that uses it
+        with torch.cuda.stream(stream):
+            return attention4(q, cache, block_table, ctx, cu_q, max_q, max_ctx, scale, causal, window, q_scale, q_zp,
+                              y_scale, y_zp, y_dtype, out, workspace)
     if q.dim() != 3:
         raise ValueError("q must be [tokens][heads][head_dim]")
     T, Hq, D = q.shape
-    B = len(ctx)
-    _here(cache.device, q=q, block_table=block_table, ctx=ctx, cu_q=cu_q, out=out, workspace=workspace)
+    B = ctx.numel()
+    _here(cache.device, q, block_table, ctx, cu_q, out, workspace)
     if q.dtype not in _FLOAT_DT:
         raise TypeError(f"q must be f16, bf16, u8 or i8, not {q.dtype}")
     _ints(ctx, "ctx")
@@ -831,15 +841,15 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
     q_ld = _heads(q, "q", (T, Hq, cache.head_dim))
     odt = q.dtype if y_dtype is None else _FLOAT_NAME[y_dtype]
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=odt, device=q.device)
-    if out.dtype != odt:
+        out = q.new_empty((T, Hq, D), dtype=odt)
+    elif out.dtype != odt:
         raise ValueError(f"out is {out.dtype}, not {odt}")
     table_ld = _table(block_table, B)
     p = AttentionParams(T, Hq, B, block_table.shape[1], q_ld, _heads(out, "out", (T, Hq, D)), table_ld, max_q, max_ctx,
                         1 if causal else 0, window, D ** -0.5 if scale is None else scale)
     need = lib().qnn_attention4_workspace_size(cache.desc, p)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = cache.data.new_empty(need)
     have = 0
     if workspace is not None:
         if not workspace.is_contiguous():
@@ -847,7 +857,7 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
         have = workspace.numel() * workspace.element_size()
     qq = _one_q(q_scale, q_zp) if q.dtype in (torch.uint8, torch.int8) else _NO_Q
     oq = _one_q(y_scale, y_zp) if odt in (torch.uint8, torch.int8) else _NO_Q
-    status = lib().qnn_attention4(_stream_handle(stream), q.data_ptr(), _FLOAT_DT[q.dtype], qq, cache.desc,
+    status = lib().qnn_attention4(_stream_handle(), q.data_ptr(), _FLOAT_DT[q.dtype], qq, cache.desc,
                                   block_table.data_ptr(), ctx.data_ptr(), None if cu_q is None else cu_q.data_ptr(),
                                   p, out.data_ptr(), _FLOAT_DT[odt], oq,
                                   None if workspace is None else workspace.data_ptr(), have)
@@ -874,28 +884,34 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.
     request b's new tokens are slots[cu[b]:cu[b + 1]], unused entries -1; status
     (a device int32) is 0, or says why nothing was changed.  All arguments are
     int32 device tensors."""
-    B = len(lens)
-    dev = lens.device
-    _here(lens.get_device(), new_lens=new_lens, block_table=block_table, free_pages=free_pages, free_count=free_count,
-          workspace=workspace)
+    if stream is not None:   # what is allocated here belongs to the stream that uses it
+        with torch.cuda.stream(stream):
+            return pages_resize(lens, new_lens, block_table, free_pages, free_count, page_size, token_capacity, workspace)
+    B = lens.numel()
+    _here(lens.get_device(), new_lens, block_table, free_pages, free_count, workspace)
     _ints(lens, "lens")
     _ints(new_lens, "new_lens", B)
     _ints(free_pages, "free_pages")
     _ints(free_count, "free_count", 1)
     ld = _table(block_table, B)
-    need = int(lib().qnn_pages_workspace_size(B))
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    elif not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
-        raise ValueError("workspace must be contiguous and of qnn_pages_workspace_size() bytes")
+    L = lib()
+    need = L.qnn_pages_workspace_size(B)
     if token_capacity < 0:
         raise ValueError("token_capacity must be >= 0")
-    out = torch.empty(B + 2 + 2 * token_capacity, dtype=torch.int32, device=dev)
-    cu, status, slots, positions = out.split_with_sizes((B + 1, 1, token_capacity, token_capacity))
-    code = lib().qnn_pages_resize(_stream_handle(stream), B, page_size, lens.data_ptr(), new_lens.data_ptr(),
-                                  block_table.data_ptr(), block_table.shape[1], ld, free_pages.data_ptr(),
-                                  free_pages.numel(), free_count.data_ptr(), cu.data_ptr(), slots.data_ptr(),
-                                  positions.data_ptr(), token_capacity, status.data_ptr(), workspace.data_ptr())
+    if workspace is None:   # one allocation with the outputs
+        work, cu, status, slots, positions = lens.new_empty(need // 4 + B + 2 + 2 * token_capacity).split_with_sizes(
+            (need // 4, B + 1, 1, token_capacity, token_capacity))
+        work = work.data_ptr()
+    else:
+        if not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
+            raise ValueError("workspace must be contiguous and of qnn_pages_workspace_size() bytes")
+        cu, status, slots, positions = lens.new_empty(B + 2 + 2 * token_capacity).split_with_sizes(
+            (B + 1, 1, token_capacity, token_capacity))
+        work = workspace.data_ptr()
+    code = L.qnn_pages_resize(_stream_handle(), B, page_size, lens.data_ptr(), new_lens.data_ptr(),
+                              block_table.data_ptr(), block_table.shape[1], ld, free_pages.data_ptr(),
+                              free_pages.numel(), free_count.data_ptr(), cu.data_ptr(), slots.data_ptr(),
+                              positions.data_ptr(), token_capacity, status.data_ptr(), work)
     if code:
         _check(code)
     return cu, slots, positions, status

@@ -233,8 +233,9 @@ def test_streams_and_repeats():
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         z = Q.attention4(**a)
+    w = Q.attention4(**a, stream=s)
     s.synchronize()
-    assert torch.equal(y, z)
+    assert torch.equal(y, z) and torch.equal(y, w)
 
 
 def test_captured_and_replayed():

@@ -140,8 +140,9 @@ def test_append_on_another_stream_and_in_a_graph():
     c = Q.Cache4(2, P, H, D, data=torch.zeros_like(ref.data))
     with torch.cuda.stream(s):
         Q.cache4_append(c, k, v, slots)
+    sk, sv = Q.cache4_read(c, slots, "f16", stream=s)
     s.synchronize()
-    assert torch.equal(c.data, ref.data)
+    assert torch.equal(c.data, ref.data) and torch.equal(sk, rk) and torch.equal(sv, rv)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         Q.cache4_append(c, k, v, slots)

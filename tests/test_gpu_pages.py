@@ -166,3 +166,17 @@ def test_captured_steps():
         torch.cuda.synchronize()
         d.compare([x.cpu().numpy() for x in got], m.resize(m.lens + 1, B), f"replay {k}")
         new += 1
+
+
+def test_on_another_stream():
+    rng = np.random.default_rng(7)
+    m = Model(40, 6, 16, 240, rng, rng.integers(0, 60, 40))
+    d = Device(m)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    new = m.lens + 3
+    arg = d.put(new)
+    torch.cuda.synchronize()
+    got = Q.pages_resize(d.lens, arg, d.table, d.stack, d.count, 16, 200, stream=s)
+    s.synchronize()
+    d.compare([x.cpu().numpy() for x in got], m.resize(new, 200), "another stream")
