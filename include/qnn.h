@@ -345,20 +345,21 @@ qnn_status qnn_cache4_read(void *stream, qnn_cache4 cache, const int32_t *slots,
  *   q: device [tokens][q_heads][head_dim], row stride q_ld, UINT8 / INT8 (q_q
  *      per tensor) or FLOAT16 / BFLOAT16; query head h reads the cache's head
  *      h / (q_heads / heads), q_heads a multiple of heads.
- *   max_q: at least the queries of any one request, and max_ctx (0: as many as
+ *   max_q: at least the queries of any one request (1 without cu_q), and max_ctx (0: as many as
  *      the table holds) about the tokens of the longest: they shape the grid.
  *      Queries past max_q are not computed; max_ctx affects the speed only.
  *   o: device [tokens][q_heads][head_dim], row stride o_ld, FLOAT16, BFLOAT16,
  *      or UINT8 / INT8 (o_q per tensor): round(o / s) + zp, ties to even,
- *      clamped to the dtype. Rows of no request (cu_q[requests] on) are left
+ *      clamped to the dtype (NaN, as from a query that is not finite: zp). Rows of no request (cu_q[requests] on) are left
  *      as they were. Must not overlap q.
  *   workspace: device, 16-byte aligned, of at least
  *      qnn_attention4_workspace_size() bytes (NULL if that is 0), read and
  *      written by this call alone until it is done; contents do not matter.
  * Rows of q and o are aligned to 8 elements (QNN_ERR_UNSUPPORTED else).
  * Scores, the softmax and sums are f32; q enters the matrix cores as f16
- * scaled by a power of two (exact for f16, and 8-bit values), each weight
- * p_t s_t as f16. Enqueued on `stream`, no synchronization.
+ * scaled by a power of two (exact for f16, bf16 and 8-bit values), each weight
+ * p_t s_t as one f16, as two where the output has 8 bits. table_width *
+ * page_size at most 2^30. Enqueued on `stream`, no synchronization.
  */
 typedef struct {
     int32_t tokens, q_heads, requests, table_width;

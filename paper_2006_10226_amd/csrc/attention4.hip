@@ -98,7 +98,8 @@ __device__ __forceinline__ Span part_of(const AttnArgs &a, Span s, int part)
     return s;
 }
 
-// A request's first query row, and its number of queries.
+// A request's first query row, and its number of queries (of which the first
+// max_q are computed).
 __device__ __forceinline__ int queries(const AttnArgs &a, int b, int *nq)
 {
     if (!a.cu) {
@@ -106,7 +107,7 @@ __device__ __forceinline__ int queries(const AttnArgs &a, int b, int *nq)
         return b;
     }
     const int first = min(max(a.cu[b], 0), a.tokens);
-    *nq = min(max(min(a.cu[b + 1], a.tokens) - first, 0), a.max_q);
+    *nq = max(min(a.cu[b + 1], a.tokens) - first, 0);
     return first;
 }
 
@@ -231,7 +232,7 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
     const int ctx = max(a.ctx[b], 0);
     int nq;
     const int first = queries(a, b, &nq);
-    const int rows = nq * a.group, row0 = tile * 16 * R;
+    const int rows = min(nq, a.max_q) * a.group, row0 = tile * 16 * R;
     if (row0 >= rows)
         return;
     const Span span = part_of(a, seen(a, ctx, nq, row0 / a.group, (min(row0 + 16 * R, rows) - 1) / a.group), part);
@@ -676,7 +677,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a, int blocks, int c
         // the parts that its tile's workgroups wrote
         const int row0 = (i * a.group + head % a.group) / (16 * blocks) * (16 * blocks);
         const Span span = seen(a, max(a.ctx[b], 0), nq, row0 / a.group,
-                               (min(row0 + 16 * blocks, nq * a.group) - 1) / a.group);
+                               (min(row0 + 16 * blocks, min(nq, a.max_q) * a.group) - 1) / a.group);
         parts = span.lo < span.hi
                     ? (int)min((int64_t)a.parts, ((int64_t)span.hi - (span.lo & ~31) + a.chunk - 1) / a.chunk)
                     : 1;
@@ -811,7 +812,7 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
                     p.tokens, p.requests, p.q_heads, p.max_q, p.max_ctx, p.window);
     if (p.q_heads % a.c.heads)
         return fail(QNN_ERR_SHAPE, "attention4: %d query heads over %d cache heads", p.q_heads, a.c.heads);
-    if (p.table_width < 1 || p.table_ld < p.table_width || (int64_t)p.table_width * cache.page_size >= (int64_t(1) << 31))
+    if (p.table_width < 1 || p.table_ld < p.table_width || (int64_t)p.table_width * cache.page_size > (int64_t(1) << 30))
         return fail(QNN_ERR_SHAPE, "attention4: table_width %d, table_ld %lld", p.table_width, (long long)p.table_ld);
     const int64_t row = (int64_t)p.q_heads * a.c.dim;
     if (p.q_ld < row || p.o_ld < row)
@@ -853,6 +854,8 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
     a.causal = p.causal != 0;
     a.window = p.window;
     a.scale = p.scale * 1.44269504088896340736f * (whole(q_dtype) ? q_q.scale[0] : 1.0f);
+    if (!std::isfinite(a.scale))
+        return fail(QNN_ERR_QPARAM, "attention4: scale times q's scale is not finite");
     a.q_zp = whole(q_dtype) ? q_q.zero_point[0] : 0;
     if (whole(o_dtype)) {
         Range r;
@@ -869,7 +872,8 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
     const int64_t unit_tiles = (g.tiles + a.stripes - 1) / a.stripes;
     const int64_t grid = g.tiles == 1 ? heads * g.parts : (heads * a.stripes + 7) / 8 * 8 * unit_tiles * g.parts;
     if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || grid >= (int64_t(1) << 31) ||
-        (int64_t)p.requests * a.max_q * p.q_heads >= (int64_t(1) << 31))
+        (int64_t)p.requests * a.max_q * p.q_heads >= (int64_t(1) << 31) ||
+        (int64_t)p.tokens * p.q_heads >= (int64_t(1) << 31))
         return fail(QNN_ERR_UNSUPPORTED, "attention4: too many row tiles");
     a.tiles = (int32_t)g.tiles;
     a.unit_tiles = (int32_t)unit_tiles;

@@ -486,7 +486,7 @@ def depthwise_conv2d_plan(x_shape, x_dtype, x_scale, x_zp, w: torch.Tensor, w_sc
                                                       _NAME_DT[y_dtype], yq.q, _clamp(act), _ROUND[rounding],
                                                       y_ldc, y_coff))
     return Plan(h, x_shape, _DT_TORCH[_NAME_DT[x_dtype]], (N, Ho, Wo, C), _DT_TORCH[_NAME_DT[y_dtype]],
-                (N, Ho, Wo, y_ldc))
+                (N, Ho, Wo, y_ldc), None if y_dtype == "i32" else (y_scale, y_zp))
 
 
 def dense_plan(M, K, x_dtype, x_scale, x_zp, w: torch.Tensor, w_scale, w_zp, bias=None, y_scale=1.0, y_zp=0,

@@ -103,7 +103,8 @@ def _attend(Q, cache=None, **kw):
     (dict(window=-1), "QNN_ERR_SHAPE"), (dict(width=0), "QNN_ERR_SHAPE"), (dict(table_ld=7), "QNN_ERR_SHAPE"),
     (dict(width=2**27, table_ld=2**27), "QNN_ERR_SHAPE"), (dict(q_ld=255), "QNN_ERR_SHAPE"),
     (dict(o_ld=128), "QNN_ERR_SHAPE"), (dict(cu=None), "QNN_ERR_SHAPE"), (dict(scale=float("nan")), "QNN_ERR_QPARAM"),
-    (dict(scale=float("inf")), "QNN_ERR_QPARAM"), (dict(qt=1, qq=(-1.0, 0)), "QNN_ERR_QPARAM"),
+    (dict(scale=float("inf")), "QNN_ERR_QPARAM"), (dict(qt=1, qq=(1e30, 0), scale=1e10), "QNN_ERR_QPARAM"),
+    (dict(tokens=2**30), "QNN_ERR_UNSUPPORTED"), (dict(width=2**26 + 1, table_ld=2**27), "QNN_ERR_SHAPE"), (dict(qt=1, qq=(-1.0, 0)), "QNN_ERR_QPARAM"),
     (dict(ot=0, oq=(0.1, 256)), "QNN_ERR_QPARAM"), (dict(q=FAKE + 8), "QNN_ERR_UNSUPPORTED"),
     (dict(o=FAKE + 4, ot=1), "QNN_ERR_UNSUPPORTED"), (dict(q_ld=260), "QNN_ERR_UNSUPPORTED"),
     (dict(o_ld=257), "QNN_ERR_UNSUPPORTED"), (dict(max_q=2**30), "QNN_ERR_UNSUPPORTED"),

@@ -177,6 +177,54 @@ def test_rows_of_no_request_stay():
     assert (out[5:] == 7).all()
 
 
+def test_queries_past_max_q_are_left():
+    """max_q below a request's queries: the first ones are computed, at their own
+    positions, the rest stays."""
+    c = Case(128, 16, 2, 4, [90, 33, 40], nq=[20, 3, 40])
+    for most in (1, 3, 17):
+        a = c.device()
+        a["max_q"] = most
+        out = torch.full(tuple(c.q.shape), 7.0, dtype=torch.float16, device="cuda")
+        y = Q.attention4(**a, out=out).cpu().double().numpy()
+        ref, tol, _ = c.expect()
+        for b in range(3):
+            lo, hi = int(c.cu[b]), int(c.cu[b + 1])
+            mid = min(hi, lo + most)
+            bound = tol[lo:mid] + np.abs(ref[lo:mid]) * _HALF_STEP["f16"] * 1.01 + 2.0**-25
+            assert (np.abs(y[lo:mid] - ref[lo:mid]) <= bound).all(), (most, b)
+            assert (y[mid:hi] == 7).all(), (most, b)
+
+
+def test_a_query_that_is_not_finite():
+    """Its own rows only; 8-bit outputs of it are the zero point."""
+    for ot in ("f16", "i8"):
+        c = Case(64, 16, 1, 4, [50, 60], ot=ot)
+        good = Q.attention4(**c.device())
+        c.q[0, 1, 5], c.q[0, 2, 63] = float("nan"), float("inf")
+        y = Q.attention4(**c.device())
+        assert torch.equal(y[0, 0], good[0, 0]) and torch.equal(y[0, 3], good[0, 3]) and torch.equal(y[1], good[1])
+        if ot == "i8":
+            assert (y[0, 1] == c.o_zp).all()
+        else:
+            assert torch.isnan(y[0, 1]).all()
+
+
+def test_workspaces():
+    """A workspace of the given size serves; a smaller one is refused."""
+    c = Case(128, 16, 1, 4, [6000, 900])
+    a = c.device()
+    y = Q.attention4(**a)
+    size = Q.attention4_workspace_size(c.c, 2, 4, 2, c.W, 1, a["max_ctx"])
+    assert size > 0
+    ws = torch.full((size + 32,), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(Q.attention4(**a, workspace=ws[:size]), y)
+    assert (ws[size:] == 255).all()
+    with pytest.raises(Q.QnnError, match="SHAPE"):
+        Q.attention4(**a, workspace=ws[:size - 16])
+    with pytest.raises(Q.QnnError, match="UNSUPPORTED"):
+        Q.attention4(**a, workspace=ws[4:4 + size])
+
+
 def test_strided_rows_and_tables():
     c = Case(128, 16, 2, 2, [90, 33, 150], nq=[4, 1, 9])
     a = c.device()
