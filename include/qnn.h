@@ -1,7 +1,7 @@
 /*
  * qnn.h -- C ABI of libqnn: quantized (INT8) conv2d, depthwise conv2d and
- * dense fused with requantize, plus standalone requantize and add, for AMD
- * Instinct MI355X (gfx950).
+ * dense fused with requantize, plus standalone requantize and add, and
+ * attention over a 4-bit cache, for AMD Instinct MI355X (gfx950).
  *
  * Problem statement (Jain et al., "Efficient Execution of Quantized Deep
  * Learning Models: A Compiler Approach"):

