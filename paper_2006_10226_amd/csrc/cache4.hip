@@ -2,9 +2,9 @@
 // neighbouring lanes per vector (a token's K or V of one head), eight channels
 // a lane. The range of a vector comes from shuffles inside its group, so each
 // input is read once and each code written once. 16384 tokens of 8 heads of 128 in
-// f16: read back 18.8 us, a copy's rate (4.5 TB/s); written 29 us (2.6 TB/s), half
-// of it issuing vector instructions (about 20 a value: range, quotient, rounding),
-// the rest the latency of slot, load and store.
+// f16, 85 MB moved: read back 18.8 us, a copy's rate (4.5 TB/s); written 22 us (3.9
+// TB/s), half of it issuing vector instructions (25 a value: conversion, range,
+// quotient, rounding, addresses), the rest the latency of load and store.
 #include "cache4.h"
 
 #include <algorithm>
@@ -55,10 +55,12 @@ __device__ __forceinline__ void load8(const void *p, float s, int z, float (&x)[
 
 // The value of another lane of the same 16 (a DPP control).
 template <int CTRL>
-__device__ __forceinline__ float lane_move(float v)
+__device__ __forceinline__ uint32_t lane_move(uint32_t v)
 {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 15, 15, true));
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 15, 15, true);
 }
+
+__device__ __forceinline__ uint32_t as_bits(float v) { return __builtin_bit_cast(uint32_t, v); }
 
 // Thread -> vector: the workgroup's 256 threads take eight consecutive tokens
 // of one head (16 for DP 64, four for 256), K and V, so that the tokens of a V
@@ -95,75 +97,104 @@ __global__ void __launch_bounds__(256) append_kernel(VecArgs a)
     const int my = threadIdx.x % kSide + threadIdx.x / (kSide * DP / 4) * kSide, my_unit = threadIdx.x / kSide % (DP / 4);
     const int my_slot = tok0 + my < a.tokens ? a.slots[tok0 + my] : -1;
     const int slot = tok < a.tokens ? a.slots[tok] : -1;
+    // the values are asked for before the slot is known: their latencies run side by side
+    const int ch = lane * 8;
+    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (tok < a.tokens && ch < a.c.dim) {
+        const int64_t off = tok * (is_v ? a.v_ld : a.k_ld) + head * a.c.dim + ch;
+        constexpr int size = DT == QNN_UINT8 || DT == QNN_INT8 ? 1 : 2;
+        load8<DT>((const uint8_t *)(is_v ? a.v : a.k) + off * size, is_v ? a.vs : a.ks, is_v ? a.vz : a.kz, x);
+    }
     uint8_t *const base = block_of(slot);
     if (base) {   // a whole group: the shuffles below stay inside one
-        const int at = slot & (P - 1), ch = lane * 8;
-        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (ch < a.c.dim) {
-            const int64_t off = tok * (is_v ? a.v_ld : a.k_ld) + head * a.c.dim + ch;
-            constexpr int size = DT == QNN_UINT8 || DT == QNN_INT8 ? 1 : 2;
-            load8<DT>((const uint8_t *)(is_v ? a.v : a.k) + off * size, is_v ? a.vs : a.ks, is_v ? a.vz : a.kz, x);
+        const int at = slot & (P - 1);
+        constexpr bool kHalf = DT == QNN_FLOAT16, kReal = kHalf || DT == QNN_BFLOAT16;
+        if constexpr (kReal) {
+            constexpr float kMost = 0x1p126f;
+            float sum = 0.0f;   // NaN, or beyond kMost, where any of the eight is
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                sum += __builtin_fabsf(x[i]);
+            if (!(sum <= kMost)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    x[i] = x[i] == x[i] ? __builtin_amdgcn_fmed3f(x[i], -kMost, kMost) : 0.0f;
+            }
         }
-        constexpr float kMost = 0x1p126f;
         float lo = 0.0f, hi = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if constexpr (DT == QNN_FLOAT16 || DT == QNN_BFLOAT16)
-                x[i] = x[i] == x[i] ? __builtin_amdgcn_fmed3f(x[i], -kMost, kMost) : 0.0f;
             lo = fminf(lo, x[i]);
             hi = fmaxf(hi, x[i]);
         }
-        // over the group: neighbours, pairs, then mirrored eights and sixteens
-        lo = fminf(lo, lane_move<0xb1>(lo));
-        hi = fmaxf(hi, lane_move<0xb1>(hi));
-        lo = fminf(lo, lane_move<0x4e>(lo));
-        hi = fmaxf(hi, lane_move<0x4e>(hi));
-        lo = fminf(lo, lane_move<0x141>(lo));
-        hi = fmaxf(hi, lane_move<0x141>(hi));
+        // Over the group: neighbours, pairs, then mirrored eights and sixteens. -lo and
+        // hi are +0 or more, so their bits compare as integers, one instruction a step
+        // (as floats, three).
+        uint32_t down = as_bits(0.0f - lo), up = as_bits(hi + 0.0f);
+        down = max(down, lane_move<0xb1>(down));
+        up = max(up, lane_move<0xb1>(up));
+        down = max(down, lane_move<0x4e>(down));
+        up = max(up, lane_move<0x4e>(up));
+        down = max(down, lane_move<0x141>(down));
+        up = max(up, lane_move<0x141>(up));
         if constexpr (M::kLanes >= 16) {
-            lo = fminf(lo, lane_move<0x140>(lo));
-            hi = fmaxf(hi, lane_move<0x140>(hi));
+            down = max(down, lane_move<0x140>(down));
+            up = max(up, lane_move<0x140>(up));
         }
         if constexpr (M::kLanes >= 32) {
-            lo = fminf(lo, __shfl_xor(lo, 16));
-            hi = fmaxf(hi, __shfl_xor(hi, 16));
+            down = max(down, (uint32_t)__shfl_xor((int)down, 16));
+            up = max(up, (uint32_t)__shfl_xor((int)up, 16));
+        }
+        float below = __builtin_bit_cast(float, down);
+        const float range = __builtin_bit_cast(float, up) + below;
+        float step;
+        if constexpr (kHalf) {   // 0, or 2^-24 and more: the remainder is exact, the quotient the correctly rounded one
+            const float q = range * (1.0f / 15.0f);
+            step = __builtin_fmaf(__builtin_fmaf(-q, 15.0f, range), 1.0f / 15.0f, q);
+        } else {
+            step = range / 15.0f;
         }
         // the scale keeps 16 significant bits, rounded up so that 15 steps span the range
-        const uint32_t sb = (__builtin_bit_cast(uint32_t, (hi - lo) / 15.0f) + 0xffu) & 0xffffff00u;
+        const uint32_t sb = (as_bits(step) + 0xffu) & 0xffffff00u;
         float s = sb ? __builtin_bit_cast(float, sb) : 1.0f;
-        if (s < 0x1p-100f) {   // the reciprocal below would overflow; exact
-            s *= 0x1p100f;
-            lo *= 0x1p100f;
+        if constexpr (!kHalf) {
+            if (s < 0x1p-100f) {   // the reciprocal below would overflow; exact
+                s *= 0x1p100f;
+                below *= 0x1p100f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                x[i] *= 0x1p100f;
+                for (int i = 0; i < 8; ++i)
+                    x[i] *= 0x1p100f;
+            }
         }
-        // x / s by the correctly rounded reciprocal and one step on the remainder,
-        // within 2^-23 of the quotient, and exact where that is a whole number and a
-        // half: 16-bit x and 16 bits of s leave no other quotient within 2^-21 of
-        // one, so the rounding is that of x / s (a full division took three times the
-        // instructions, which bound the kernel)
-        const float inv = 1.0f / s;
+        // x / s by a reciprocal within 2^-23 and one step on the remainder: that is
+        // exact (16 bits of s, and q's error is 2^-22 of it), so the result is the
+        // quotient, off by 2^-44, rounded once: exact where the quotient is a whole
+        // number and a half. 16-bit x and 16 bits of s leave no other quotient within
+        // 2^-21 of one, so the rounding is that of x / s (divisions took three times
+        // the instructions, which bound the kernel).
+        const float inv = __builtin_amdgcn_rcpf(s);
         auto steps = [&](float v) {
             const float q = v * inv;
             return __builtin_rintf(__builtin_fmaf(__builtin_fmaf(-q, s, v), inv, q));
         };
-        const float z = fminf(steps(-lo), 15.0f);
-        uint32_t c[8];
+        const float z = fminf(steps(below), 15.0f);
+        float c[8];   // the codes less z
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            c[i] = (uint32_t)__builtin_amdgcn_fmed3f(steps(x[i]) + z, 0.0f, 15.0f);
+            c[i] = __builtin_amdgcn_fmed3f(steps(x[i]), -z, 15.0f - z);
+        // four codes as the digits of a number to base 16, exact in f32
+        auto four = [&](float c0, float c1, float c2, float c3) {
+            const float high = __builtin_fmaf(c3, 16.0f, c2), low = __builtin_fmaf(c1, 16.0f, c0);
+            return (uint32_t)__builtin_fmaf(high, 256.0f, __builtin_fmaf(z, 0x1111, low));
+        };
         if (!is_v) {
-            uint32_t w = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w |= c[2 * i] << (4 * i) | c[2 * i + 1] << (16 + 4 * i);
-            *(uint32_t *)(base + at * (DP / 2) + lane * 4) = w;
+            *(uint32_t *)(base + at * (DP / 2) + lane * 4) =
+                four(c[0], c[2], c[4], c[6]) | four(c[1], c[3], c[5], c[7]) << 16;
         } else {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 unit[vec - M::kTokens][lane * 2 + u] =
-                    (uint16_t)(c[4 * u] | c[4 * u + 1] << 4 | c[4 * u + 2] << 8 | c[4 * u + 3] << 12);
+                    (uint16_t)four(c[4 * u], c[4 * u + 1], c[4 * u + 2], c[4 * u + 3]);
         }
         if (lane == 0)
             *(uint32_t *)(base + P * DP + (is_v ? 4 * P : 0) + at * 4) = sb | (uint32_t)z;

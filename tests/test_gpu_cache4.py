@@ -152,3 +152,38 @@ def test_append_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(c.data, ref.data) and torch.equal(gk, rk) and torch.equal(gv, rv)
+
+
+@pytest.mark.parametrize("dtype,low,high", [("f16", -24, 15), ("bf16", -133, 126), ("i8", 0, 0), ("u8", 0, 0)])
+def test_append_codes_and_records_over_all_ranges(dtype, low, high):
+    """Every code and record of 20000 vectors: their ranges over the type's, a third
+    of them small integers times one step, so that quotients fall on halves."""
+    T, D, P = 20000, 64, 64
+    rng = np.random.default_rng(T + high)
+    if dtype in ("i8", "u8"):
+        first = -128 if dtype == "i8" else 0
+        x = np.clip(rng.integers(-9, 10, (T, 1, D)) * rng.integers(1, 15, (T, 1, 1)) + rng.integers(0, 100, (T, 1, 1)),
+                    first, first + 255)
+        scale, zp = np.float32(0.037), 3
+        val = (x - zp).astype(np.float32) * scale
+        x = torch.from_numpy(x.astype(np.int16)).to(_TORCH[dtype])
+    else:
+        v = rng.normal(rng.normal(size=(T, 1, 1)), 1, (T, 1, D))
+        v[::3] = rng.integers(-rng.integers(1, 30, (T, 1, 1))[::3], 31, v[::3].shape) / 8
+        v *= 2.0 ** rng.integers(low, high - 3, (T, 1, 1))
+        x = torch.from_numpy(v).to(_TORCH[dtype])
+        scale, zp, val = 1.0, 0, x.float().numpy()
+    pages = -(-T // P)
+    c = Q.Cache4(pages, P, 1, D, data=torch.full((pages, R.page_bytes(P, 1, D)), 255, dtype=torch.uint8, device="cuda"))
+    Q.cache4_append(c, x.cuda(), x.cuda(), torch.arange(T, dtype=torch.int32, device="cuda"), scale, zp, scale, zp)
+    got = c.data.cpu().numpy()
+    code, s, z = R.quantize(val[:, 0])
+    rec = s.view(np.uint32) | z
+    for kind, place in enumerate((R.k_place, R.v_place)):
+        byte, shift = place(P, D)
+        have = (got[:, byte] >> shift & 15).reshape(-1, D)[:T]
+        at = P * D + 4 * P * kind
+        have_rec = got[:, at:at + 4 * P].copy().view(np.uint32).reshape(-1)[:T]
+        assert np.array_equal(have_rec, rec), (kind, np.flatnonzero(have_rec != rec)[:4])
+        bad = np.argwhere(have != code)
+        assert bad.size == 0, (kind, len(bad), bad[:4].tolist())
