@@ -97,15 +97,15 @@ __global__ void __launch_bounds__(256) append_kernel(VecArgs a)
     const int my = threadIdx.x % kSide + threadIdx.x / (kSide * DP / 4) * kSide, my_unit = threadIdx.x / kSide % (DP / 4);
     const int my_slot = tok0 + my < a.tokens ? a.slots[tok0 + my] : -1;
     const int slot = tok < a.tokens ? a.slots[tok] : -1;
-    // the values are asked for before the slot is known: their latencies run side by side
+    uint8_t *const base = block_of(slot);
+    // a skipped token's rows may not exist: nothing is loaded before its slot is known
     const int ch = lane * 8;
     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (tok < a.tokens && ch < a.c.dim) {
+    if (base && ch < a.c.dim) {
         const int64_t off = tok * (is_v ? a.v_ld : a.k_ld) + head * a.c.dim + ch;
         constexpr int size = DT == QNN_UINT8 || DT == QNN_INT8 ? 1 : 2;
         load8<DT>((const uint8_t *)(is_v ? a.v : a.k) + off * size, is_v ? a.vs : a.ks, is_v ? a.vz : a.kz, x);
     }
-    uint8_t *const base = block_of(slot);
     if (base) {   // a whole group: the shuffles below stay inside one
         const int at = slot & (P - 1);
         constexpr bool kHalf = DT == QNN_FLOAT16, kReal = kHalf || DT == QNN_BFLOAT16;
