@@ -313,6 +313,7 @@ size_t qnn_cache4_page_bytes(int32_t page_size, int32_t heads, int32_t head_dim)
  * s = (hi - lo) / 15, rounded up to a 16-bit significand, z = round(-lo / s),
  * c = clamp(round(x / s) + z, 0, 15), ties to even; a vector of zeros has
  * s = 0. NaN counts as 0, and values beyond +-2^126 as that.
+ * tokens * heads * DP below 2^34 (a launch's size; QNN_ERR_UNSUPPORTED else).
  * Enqueued on `stream`, no synchronization.
  */
 qnn_status qnn_cache4_append(void *stream, qnn_cache4 cache, const void *k, const void *v, qnn_dtype dtype,
@@ -323,7 +324,7 @@ qnn_status qnn_cache4_append(void *stream, qnn_cache4 cache, const void *k, cons
  * Reads the vectors at slots[i] back as s * (c - z), rounded to dtype
  * (FLOAT16 or BFLOAT16): element (i, h, d) at i * ld + h * head_dim + d. Slots
  * below 0 or past the last page give zeros. k or v may be NULL: not read.
- * Enqueued on `stream`, no synchronization.
+ * tokens * heads * DP as for the append. Enqueued on `stream`, no synchronization.
  */
 qnn_status qnn_cache4_read(void *stream, qnn_cache4 cache, const int32_t *slots, int32_t tokens, void *k, void *v,
                            qnn_dtype dtype, int64_t k_ld, int64_t v_ld);
@@ -359,7 +360,10 @@ qnn_status qnn_cache4_read(void *stream, qnn_cache4 cache, const int32_t *slots,
  * Scores, the softmax and sums are f32; q enters the matrix cores as f16
  * scaled by a power of two (exact for f16, bf16 and 8-bit values), each weight
  * p_t s_t as one f16, as two where the output has 8 bits. table_width *
- * page_size at most 2^30. Enqueued on `stream`, no synchronization.
+ * page_size at most 2^30. The grid has a workgroup for 32 rows (of max_q *
+ * q_heads / heads) of every request and cache head, and takes fewer than 2^24 of
+ * them (QNN_ERR_UNSUPPORTED else: fewer requests a call, or max_q nearer to their
+ * queries). Enqueued on `stream`, no synchronization.
  */
 typedef struct {
     int32_t tokens, q_heads, requests, table_width;

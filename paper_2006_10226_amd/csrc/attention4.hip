@@ -879,7 +879,9 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
     a.stripes = g.tiles == 1 ? 1 : heads % 8 == 0 ? 1 : heads % 4 == 0 ? 2 : heads % 2 == 0 ? 4 : 8;
     const int64_t unit_tiles = (g.tiles + a.stripes - 1) / a.stripes;
     const int64_t grid = g.tiles == 1 ? heads * g.parts : (heads * a.stripes + 7) / 8 * 8 * unit_tiles * g.parts;
-    if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || grid >= (int64_t(1) << 31) ||
+    // a launch takes fewer than 2^32 threads (the join's are far fewer: it follows grids
+    // below shape_of's `want` only)
+    if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || grid >= (int64_t(1) << 32) / (kWaves * 64) ||
         (int64_t)p.requests * a.max_q * p.q_heads >= (int64_t(1) << 31) ||
         (int64_t)p.tokens * p.q_heads >= (int64_t(1) << 31))
         return fail(QNN_ERR_UNSUPPORTED, "attention4: too many row tiles");

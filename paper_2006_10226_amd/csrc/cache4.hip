@@ -301,9 +301,11 @@ qnn_status check_rows(const char *what, const void *p, int64_t ld, const Cache4A
     return QNN_OK;
 }
 
+// A launch takes fewer than 2^32 threads.
 qnn_status check_grid(const char *what, int32_t tokens, const Cache4Args &c)
 {
-    if (((int64_t)tokens + 3) / 4 * c.heads >= (int64_t(1) << 31))
+    const int per = 1024 / cache4_padded(c.dim);   // Map<DP>::kTokens
+    if (((int64_t)tokens + per - 1) / per * c.heads >= (int64_t(1) << 32) / 256)
         return fail(QNN_ERR_UNSUPPORTED, "%s: too many vectors in one call", what);
     return QNN_OK;
 }
