@@ -756,6 +756,15 @@ Shape shape_of(const qnn_attention_params &p, int group, int heads, int page_siz
     return s;
 }
 
+// Whether 32 bits hold the rows of a call of at most max_q queries a request; the
+// sums of shape_of and the join's row numbers rely on it.
+bool countable(const qnn_attention_params &p, int64_t max_q)
+{
+    constexpr int64_t kMost = int64_t(1) << 31;
+    return (int64_t)p.tokens * p.q_heads < kMost && max_q * p.q_heads < kMost &&
+           max_q * p.q_heads * p.requests < kMost;
+}
+
 size_t parts_bytes(const Shape &s, const qnn_attention_params &p, int dp)
 {
     return s.parts == 1 ? 0 : (size_t)s.parts * p.tokens * p.q_heads * (dp * sizeof(float) + sizeof(float2));
@@ -799,8 +808,11 @@ size_t qnn_attention4_workspace_size(qnn_cache4 cache, qnn_attention_params p)
         return 0;
     // the same for calls with cu_q and without (one query each): the larger
     const int group = p.q_heads / cache.heads, dp = cache4_padded(cache.head_dim);
-    return std::max(parts_bytes(shape_of(p, group, cache.heads, cache.page_size, true), p, dp),
-                    parts_bytes(shape_of(p, group, cache.heads, cache.page_size, false), p, dp));
+    size_t most = 0;
+    for (const bool packed : {true, false})
+        if (countable(p, packed ? p.max_q : 1))
+            most = std::max(most, parts_bytes(shape_of(p, group, cache.heads, cache.page_size, packed), p, dp));
+    return most;
 }
 
 qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qparams q_q, qnn_cache4 cache,
@@ -841,6 +853,8 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
     const int q_size = whole(q_dtype) ? 1 : 2, o_size = whole(o_dtype) ? 1 : 2;
     if (p.q_ld % 8 || p.o_ld % 8 || ((uintptr_t)q & (8 * q_size - 1)) || ((uintptr_t)o & (8 * o_size - 1)))
         return fail(QNN_ERR_UNSUPPORTED, "attention4: rows of q and o must be aligned to 8 elements");
+    if (!countable(p, cu_q ? p.max_q : 1))
+        return fail(QNN_ERR_UNSUPPORTED, "attention4: too many row tiles");
     if (qnn_attention4_workspace_size(cache, p) > workspace_bytes)
         return fail(QNN_ERR_SHAPE, "attention4: the workspace is smaller than qnn_attention4_workspace_size()");
     a.q = q;
@@ -881,9 +895,7 @@ qnn_status qnn_attention4(void *stream, const void *q, qnn_dtype q_dtype, qnn_qp
     const int64_t grid = g.tiles == 1 ? heads * g.parts : (heads * a.stripes + 7) / 8 * 8 * unit_tiles * g.parts;
     // a launch takes fewer than 2^32 threads (the join's are far fewer: it follows grids
     // below shape_of's `want` only)
-    if ((int64_t)a.max_q * a.group >= (int64_t(1) << 31) || grid >= (int64_t(1) << 32) / (kWaves * 64) ||
-        (int64_t)p.requests * a.max_q * p.q_heads >= (int64_t(1) << 31) ||
-        (int64_t)p.tokens * p.q_heads >= (int64_t(1) << 31))
+    if (grid >= (int64_t(1) << 32) / (kWaves * 64))
         return fail(QNN_ERR_UNSUPPORTED, "attention4: too many row tiles");
     a.tiles = (int32_t)g.tiles;
     a.unit_tiles = (int32_t)unit_tiles;
