@@ -109,8 +109,8 @@ __global__ void __launch_bounds__(256) append_kernel(VecArgs a)
     if (base) {   // a whole group: the shuffles below stay inside one
         const int at = slot & (P - 1);
         constexpr bool kHalf = DT == QNN_FLOAT16, kReal = kHalf || DT == QNN_BFLOAT16;
+        constexpr float kMost = 0x1p126f;
         if constexpr (kReal) {
-            constexpr float kMost = 0x1p126f;
             float sum = 0.0f;   // NaN, or beyond kMost, where any of the eight is
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -120,6 +120,10 @@ __global__ void __launch_bounds__(256) append_kernel(VecArgs a)
                 for (int i = 0; i < 8; ++i)
                     x[i] = x[i] == x[i] ? __builtin_amdgcn_fmed3f(x[i], -kMost, kMost) : 0.0f;
             }
+        } else if ((is_v ? a.vs : a.ks) > kMost / 256.0f) {   // of 255 steps at most
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                x[i] = __builtin_amdgcn_fmed3f(x[i], -kMost, kMost);
         }
         float lo = 0.0f, hi = 0.0f;
 #pragma unroll
@@ -169,9 +173,10 @@ __global__ void __launch_bounds__(256) append_kernel(VecArgs a)
         // x / s by a reciprocal within 2^-23 and one step on the remainder: that is
         // exact (16 bits of s, and q's error is 2^-22 of it), so the result is the
         // quotient, off by 2^-44, rounded once: exact where the quotient is a whole
-        // number and a half. 16-bit x and 16 bits of s leave no other quotient within
-        // 2^-21 of one, so the rounding is that of x / s (divisions took three times
-        // the instructions, which bound the kernel).
+        // number and a half. Other quotients (of a 16-bit x or of a product's 24 bits, and
+        // 16 bits of s) are at least 2^-41 of themselves from where a rounding changes,
+        // so the rounding is that of x / s (divisions took three times the
+        // instructions, which bound the kernel).
         const float inv = __builtin_amdgcn_rcpf(s);
         auto steps = [&](float v) {
             const float q = v * inv;
