@@ -22,7 +22,9 @@
 //   one row, which is exactly the operand that
 //   o^T [channel][row] += V^T p^T wants: the weights never leave the lane.
 // The running offset u of a row is raised only when a weight would leave
-// f16's or a sum f32's comfortable range (w > 2^8 or sum p > 2^98); the
+// f16's or a sum f32's comfortable range (w > 2^15 or sum p > 2^98), and then
+// so that the largest weight is 2^7: f16 holds weights down to 2^-31 of it, so
+// that a token which outweighs a long tail takes little of the tail's sum. The
 // output is linear in the weights, so any u gives the same quotient.
 //
 // The four waves of a workgroup take every fourth 32 tokens and are joined
@@ -77,7 +79,7 @@ struct AttnArgs {
 constexpr int kWaves = 4;
 constexpr uint32_t kCode = 0x00f000f0u;   // a code at bits 4 .. 7 of each half: c * 2^-20
 constexpr float kNone = -1e30f;      // offset of a row without tokens yet
-constexpr float kMaxWeight = 256.0f, kMaxSum = 0x1p98f;
+constexpr float kMaxWeight = 0x1p15f, kMaxSum = 0x1p98f;
 
 // Tokens [lo, hi) that rows first .. last - 1 of a request see between them; a
 // row is a query (row / group) and one of the heads.
@@ -449,13 +451,13 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
             };
             weigh();
             if (__any(top > kMaxWeight || sum > kMaxSum)) {
-                // raise the offset: the largest weight becomes 1 (or, where V's scales
-                // are below 2^-90, the largest p 2^90)
+                // raise the offset: the largest weight becomes 2^7 (or, where V's scales
+                // are below 2^-83, the largest p 2^90)
                 float most = kNone;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float x = sc[r][j >> 2][j & 3] * fac[r];
-                    most = fmaxf(most, fmaxf(x + __builtin_amdgcn_logf(vs[j]), x - 90.0f));
+                    most = fmaxf(most, fmaxf(x + (__builtin_amdgcn_logf(vs[j]) - 7.0f), x - 90.0f));
                 }
                 most = fmaxf(row_max(most), off[r]);
                 const float down = __builtin_amdgcn_exp2f(off[r] - most);
@@ -471,7 +473,7 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
             h8 h;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                h[j] = (_Float16)w[j];   // rounded to nearest: 2^-11 of each weight at most, in no direction
+                h[j] = (_Float16)w[j];   // rounded to nearest: 2^-11 of each weight, or 2^-25, at most
             pw[r] = __builtin_bit_cast(u4, h);
             if constexpr (FINE) {
                 h8 l;
