@@ -80,6 +80,7 @@ constexpr int kWaves = 4;
 constexpr uint32_t kCode = 0x00f000f0u;   // a code at bits 4 .. 7 of each half: c * 2^-20
 constexpr float kNone = -1e30f;      // offset of a row without tokens yet
 constexpr float kMaxWeight = 0x1p15f, kMaxSum = 0x1p98f;
+constexpr float kFar = 0x1p14f;      // offsets beyond it are rounded by up to 2^-10 and more
 
 // Tokens [lo, hi) that rows first .. last - 1 of a request see between them; a
 // row is a query (row / group) and one of the heads.
@@ -437,22 +438,20 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
         u4 pw[R], pl[FINE ? R : 1];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float p[8], w[8], sum, top;
-            auto weigh = [&]() {
-                sum = 0.0f;
-                top = 0.0f;
+            float w[8], sum = 0.0f, top = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r][j >> 2][j & 3], fac[r], -off[r]));
-                    w[j] = p[j] * vs[j];
-                    sum += p[j];
-                    top = fmaxf(top, w[j]);
-                }
-            };
-            weigh();
-            if (__any(top > kMaxWeight || sum > kMaxSum)) {
+            for (int j = 0; j < 8; ++j) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r][j >> 2][j & 3], fac[r], -off[r]));
+                w[j] = p * vs[j];
+                sum += p;
+                top = fmaxf(top, w[j]);
+            }
+            if (__any(top > kMaxWeight || sum > kMaxSum || fabsf(off[r]) > kFar)) {
                 // raise the offset: the largest weight becomes 2^7 (or, where V's scales
-                // are below 2^-83, the largest p 2^90)
+                // are below 2^-83, the largest p 2^90). The scores are rounded before the
+                // offset, a rounded one, is taken off: the unrounded one above may differ
+                // from it by half a step, which beside 2^27 is 2^3.
+#pragma clang fp contract(off)
                 float most = kNone;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -467,7 +466,13 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
                     acc[r][j] *= down;
-                weigh();
+                sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(sc[r][j >> 2][j & 3] * fac[r] - most);
+                    w[j] = p * vs[j];
+                    sum += p;
+                }
             }
             total[r] += sum;
             h8 h;

@@ -1,6 +1,6 @@
 """Attention over the 4-bit cache where its numbers are far apart: a token that
-outweighs a long tail. Keys and values are written by qnn_cache4_append and known
-exactly, so that the softmax is too."""
+outweighs a long tail, scores of any size. Keys and values are written by
+qnn_cache4_append and known exactly, so that the softmax is too."""
 import math
 
 import numpy as np
@@ -65,3 +65,26 @@ def test_a_token_before_a_long_flat_tail(ot, tail):
     else:
         tol = tol + want * _HALF_STEP[ot]
     assert (np.abs(y[0] - want) <= tol).all(), (y[0, :3], want[:3], tol[:3])
+
+
+def _means(v, ot):
+    want = v.mean(0)
+    # equal weights; f16 values of them, f32 sums of a few dozen
+    return want, np.abs(v).max(0) * 2.0**-18 + np.abs(want) * (2.0**-11 + _HALF_STEP[ot])
+
+
+@pytest.mark.parametrize("power", [10, 20, 24, 30, 60])
+def test_scores_of_any_size(power):
+    """Two tokens share the highest score, of up to 2^95; all others are far behind."""
+    T, D = 200, 64
+    rng = np.random.default_rng(power)
+    k = np.zeros((T, D), np.float32)
+    k[:, 0] = rng.integers(1, 5, T) * 2.0**power
+    k[[31, 150], 0] = 8 * 2.0**power
+    v = rng.integers(-8, 9, (T, D)).astype(np.float32)
+    c, (_, vs), table = _cache(k, v)
+    q = torch.zeros(64, D, dtype=torch.bfloat16)
+    q[:, 0] = 2.0**min(power, 30) * (1 + torch.arange(64) / 64)
+    y = _attend(c, table, T, q, scale=0.125)
+    want, tol = _means(vs[[31, 150]], "bf16")
+    assert (np.abs(y - want) <= tol).all(), np.abs(y - want).max()
