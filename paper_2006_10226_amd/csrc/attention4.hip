@@ -78,7 +78,7 @@ struct AttnArgs {
 
 constexpr int kWaves = 4;
 constexpr uint32_t kCode = 0x00f000f0u;   // a code at bits 4 .. 7 of each half: c * 2^-20
-constexpr float kNone = -1e30f;      // offset of a row without tokens yet
+constexpr float kNone = -0x1.fffffep127f;   // offset of a row without tokens yet: no score is below
 constexpr float kMaxWeight = 0x1p15f, kMaxSum = 0x1p98f;
 constexpr float kFar = 0x1p14f;      // offsets beyond it are rounded by up to 2^-10 and more
 

@@ -88,3 +88,19 @@ def test_scores_of_any_size(power):
     y = _attend(c, table, T, q, scale=0.125)
     want, tol = _means(vs[[31, 150]], "bf16")
     assert (np.abs(y - want) <= tol).all(), np.abs(y - want).max()
+
+
+@pytest.mark.parametrize("power", [3, 40, 59])
+def test_scores_far_below_zero(power):
+    """All tokens at one score, down to -2^118."""
+    T, D = 64, 64
+    rng = np.random.default_rng(power)
+    k = np.zeros((T, D), np.float32)
+    k[:, 0] = 2.0**power
+    v = rng.integers(-8, 9, (T, D)).astype(np.float32)
+    c, (_, vs), table = _cache(k, v)
+    q = torch.zeros(3, D, dtype=torch.bfloat16)
+    q[:, 0] = -(2.0**power) * torch.tensor([1.0, 1.25, 1.5])
+    y = _attend(c, table, T, q, scale=0.125)
+    want, tol = _means(vs, "bf16")
+    assert (np.abs(y - want) <= tol).all(), np.abs(y - want).max()
