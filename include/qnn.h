@@ -358,7 +358,8 @@ qnn_status qnn_cache4_read(void *stream, qnn_cache4 cache, const int32_t *slots,
  *      written by this call alone until it is done; contents do not matter.
  * Rows of q and o are aligned to 8 elements (QNN_ERR_UNSUPPORTED else).
  * Scores, the softmax and sums are f32; q enters the matrix cores as f16
- * scaled by a power of two (exact for f16, bf16 and 8-bit values), each weight
+ * scaled by a power of two (exact for 8-bit values and for f16 and bf16 ones down
+ * to 2^-28 of the row's largest; scale * q counts up to 2^121), each weight
  * p_t s_t as one f16, as two where the output has 8 bits. table_width *
  * page_size at most 2^30. The grid has a workgroup for 32 rows (of max_q *
  * q_heads / heads) of every request and cache head, and takes fewer than 2^24 of

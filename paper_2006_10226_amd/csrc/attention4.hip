@@ -375,8 +375,10 @@ __global__ void __launch_bounds__(kWaves * 64, (wave_target<DP, R>())) attention
             q[r][k] = __builtin_bit_cast(u4, h8v);
         }
         qsum[r] = row_sum(sum) * 0x1p-20f;
-        // least above 0, so that a masked score (-inf) stays one
-        fac[r] = fmaxf(fabsf(a.scale) * 0x1p20f / up, 0x1p-126f);
+        // above 0, so that a masked score (-inf) stays one, and finite, so that a score
+        // of 0 does: the largest f32 stands for what a row of 2^121 and more (scale
+        // included) would have
+        fac[r] = fminf(fmaxf(fabsf(a.scale) * 0x1p20f / up, 0x1p-126f), 0x1.fffffep127f);
     }
 
     f4 acc[R][NV], zacc[R];

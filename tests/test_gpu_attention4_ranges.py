@@ -1,6 +1,6 @@
 """Attention over the 4-bit cache where its numbers are far apart: a token that
-outweighs a long tail, scores of any size. Keys and values are written by
-qnn_cache4_append and known exactly, so that the softmax is too."""
+outweighs a long tail, scores of any size, queries of any size. Keys and values
+are written by qnn_cache4_append and known exactly, so that the softmax is too."""
 import math
 
 import numpy as np
@@ -101,6 +101,19 @@ def test_scores_far_below_zero(power):
     c, (_, vs), table = _cache(k, v)
     q = torch.zeros(3, D, dtype=torch.bfloat16)
     q[:, 0] = -(2.0**power) * torch.tensor([1.0, 1.25, 1.5])
+    y = _attend(c, table, T, q, scale=0.125)
+    want, tol = _means(vs, "bf16")
+    assert (np.abs(y - want) <= tol).all(), np.abs(y - want).max()
+
+
+@pytest.mark.parametrize("size", [1e-38, 1e30, 1e36, 3e38])
+def test_queries_of_any_size_on_keys_of_zero(size):
+    T, D = 64, 64
+    rng = np.random.default_rng(7)
+    v = rng.integers(-8, 9, (T, D)).astype(np.float32)
+    c, (_, vs), table = _cache(np.zeros((T, D), np.float32), v)
+    q = (torch.from_numpy(rng.uniform(-1, 1, (3, D))) * size).to(torch.bfloat16)
+    q[:, 0] = size
     y = _attend(c, table, T, q, scale=0.125)
     want, tol = _means(vs, "bf16")
     assert (np.abs(y - want) <= tol).all(), np.abs(y - want).max()
