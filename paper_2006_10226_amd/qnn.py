@@ -727,11 +727,13 @@ def _heads(t: torch.Tensor, name: str, shape) -> int:
     if t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
     T, H, D = shape
+    if T == 0:
+        return H * D
     row, head, one = t.stride()
     if D > 1 and one != 1 or H > 1 and head != D:
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    if T <= 1:
-        return max(H * D, row)
+    if T == 1:
+        return H * D
     if row < H * D:
         raise ValueError(f"{name}: rows overlap (stride {row})")
     return row
