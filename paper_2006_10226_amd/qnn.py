@@ -814,7 +814,7 @@ def cache4_read(cache: Cache4, slots: torch.Tensor, dtype="f16", stream=None) ->
 
 
 def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: torch.Tensor,
-               cu_q: Optional[torch.Tensor] = None, max_q: int = 1, max_ctx: int = 0, scale: Optional[float] = None,
+               cu_q: Optional[torch.Tensor] = None, max_q: Optional[int] = None, max_ctx: int = 0, scale: Optional[float] = None,
                causal=True, window: int = 0, q_scale=1.0, q_zp=0, y_scale=1.0, y_zp=0, y_dtype: Optional[str] = None,
                out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                stream=None) -> torch.Tensor:
@@ -822,7 +822,9 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
     q_scale and q_zp) over the cache; see qnn_attention4.  Request b's queries
     are rows cu_q[b] .. cu_q[b + 1] - 1 (cu_q None: one each), the last of its
     ctx[b] tokens; block_table is int32 [requests][pages].  max_q is at least any
-    request's queries, max_ctx (0: unknown) about the longest ctx.  scale
+    request's queries, the rest of which stays uncomputed (None: that isn't known,
+    all of q, for which the grid is that much larger), max_ctx (0: unknown) about
+    the longest ctx.  scale
     defaults to head_dim ** -0.5.  The output has y_dtype ("f16", "bf16", "u8",
     "i8"; q's by default), 8-bit ones with y_scale and y_zp.  `workspace` is a
     uint8 tensor of attention4_workspace_size() bytes, allocated here if not
@@ -847,6 +849,8 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
     elif out.dtype != odt:
         raise ValueError(f"out is {out.dtype}, not {odt}")
     table_ld = _table(block_table, B)
+    if max_q is None:
+        max_q = 1 if cu_q is None else max(T, 1)
     p = AttentionParams(T, Hq, B, block_table.shape[1], q_ld, _heads(out, "out", (T, Hq, D)), table_ld, max_q, max_ctx,
                         1 if causal else 0, window, D ** -0.5 if scale is None else scale)
     need = lib().qnn_attention4_workspace_size(cache.desc, p)
@@ -869,8 +873,10 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
 
 
 def attention4_workspace_size(cache: Cache4, tokens: int, q_heads: int, requests: int, table_width: int,
-                              max_q: int = 1, max_ctx: int = 0, causal=True, window: int = 0) -> int:
+                              max_q: Optional[int] = None, max_ctx: int = 0, causal=True, window: int = 0) -> int:
     """Bytes of workspace of attention4 calls of these sizes (0: none)."""
+    if max_q is None:
+        max_q = max(tokens, 1)
     ld = q_heads * cache.head_dim
     p = AttentionParams(tokens, q_heads, requests, table_width, ld, ld, table_width, max_q, max_ctx, int(bool(causal)),
                         window, 1.0)
