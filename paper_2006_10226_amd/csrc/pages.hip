@@ -121,10 +121,13 @@ __device__ __forceinline__ Head sum_requests(const PagesArgs &a, Lists *lists)
     T gone = 0, got = 0, add = 0;
     int bad = n < 0 || n > a.capacity, old = 0, now = 0;
     Sums<T> s{0, 0, 0};
-    for (int at = 0; at < a.requests; at += kSumThreads) {
-        const int b = at + tid;
+    // (counts are below 2^31 and numbers unsigned, here and below: the one past the
+    // last, by a stride, doesn't wrap)
+    const uint32_t requests = (uint32_t)a.requests;
+    for (uint32_t at = 0; at < requests; at += kSumThreads) {
+        const uint32_t b = at + tid;
         Sums<T> v{0, 0, 0};
-        if (b < a.requests) {
+        if (b < requests) {
             old = a.lens[b];
             now = a.new_lens[b];
             if (old < 0 || now < 0 || old > most || now > most) {
@@ -136,7 +139,7 @@ __device__ __forceinline__ Head sum_requests(const PagesArgs &a, Lists *lists)
         }
         Sums<T> total;
         s = block_scan<T>(v, &total);
-        if (!LISTS && b < a.requests) {
+        if (!LISTS && b < requests) {
             // a sum beyond 32 bits is refused below, by its total
             a.old[b] = old;
             a.gone[b] = (int)(gone + s.gone);
@@ -169,7 +172,7 @@ __device__ __forceinline__ Head sum_requests(const PagesArgs &a, Lists *lists)
                 a.lens[tid] = now;
         }
     } else {
-        for (int b = tid; b < a.requests; b += kSumThreads) {
+        for (uint32_t b = tid; b < requests; b += kSumThreads) {
             if (status)
                 a.cu[b] = 0;
             else
@@ -194,11 +197,11 @@ __device__ __forceinline__ Head sum_requests(const PagesArgs &a, Lists *lists)
 
 // Pages given back: element `at` on, by `stride`.
 template <typename G, typename N>
-__device__ __forceinline__ void give_back(const PagesArgs &a, const Head &h, const G &gone, const N &now, int at,
-                                          int stride)
+__device__ __forceinline__ void give_back(const PagesArgs &a, const Head &h, const G &gone, const N &now, uint32_t at,
+                                          uint32_t stride)
 {
-    for (int i = at; i < h.gone; i += stride) {
-        const int b = find(gone, a.requests, i);
+    for (uint32_t n = at; n < (uint32_t)h.gone; n += stride) {
+        const int i = (int)n, b = find(gone, a.requests, i);
         int32_t *entry = a.table + b * a.ld + pages_of(now[b], a.shift) + (i - gone[b]);
         a.free_pages[h.count - 1 - i] = *entry;
         *entry = -1;
@@ -208,9 +211,10 @@ __device__ __forceinline__ void give_back(const PagesArgs &a, const Head &h, con
 // Slots, positions and new table entries: tokens `at` on, by `stride`.
 template <typename C, typename O, typename G>
 __device__ __forceinline__ void place_tokens(const PagesArgs &a, const Head &h, const C &cu, const O &olds, const G &got,
-                                             int at, int stride)
+                                             uint32_t at, uint32_t stride)
 {
-    for (int t = at; t < a.tokens; t += stride) {
+    for (uint32_t n = at; n < (uint32_t)a.tokens; n += stride) {
+        const int t = (int)n;
         int slot = -1, pos = 0;
         if (t < h.tokens) {
             const int b = find(cu, a.requests, t);
