@@ -694,8 +694,15 @@ _FLOAT_NAME = {"u8": torch.uint8, "i8": torch.int8, "f16": torch.float16, "bf16"
 _NO_Q = QParams(None, None, 0)
 
 
+def _i32(*values):
+    """Numbers that become C ints: ctypes cuts longer ones off without a word."""
+    if max(values) > INT32_MAX or min(values) < INT32_MIN:
+        raise ValueError(f"{[v for v in values if not INT32_MIN <= v <= INT32_MAX]} does not fit 32 bits")
+
+
 def _one_q(scale, zp) -> QParams:
     """Per-tensor qparams of two numbers (a tenth of _Q's time, which small calls see)."""
+    _i32(zp)
     return QParams(ctypes.pointer(ctypes.c_float(scale)), ctypes.pointer(ctypes.c_int32(zp)), 1)
 
 
@@ -759,6 +766,7 @@ class Cache4:
 
     def __init__(self, num_pages: int, page_size: int, heads: int, head_dim: int, device="cuda",
                  data: Optional[torch.Tensor] = None):
+        _i32(num_pages, page_size, heads, head_dim)
         per_page = int(lib().qnn_cache4_page_bytes(page_size, heads, head_dim))
         if per_page == 0 or num_pages < 1:
             raise ValueError(f"no cache of {num_pages} pages of {page_size} tokens, {heads} heads of {head_dim}: "
@@ -781,6 +789,7 @@ def cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, slots: torch.
     their scale and zero point) to 4 bits at `slots` (int32; below 0: skipped);
     see qnn_cache4_append.  k and v may be slices of a wider tensor of rows."""
     T = k.shape[0]
+    _i32(T)
     _here(cache.device, k, v, slots)
     if k.dtype not in _FLOAT_DT or v.dtype != k.dtype:
         raise TypeError(f"k and v must both be f16, bf16, u8 or i8, not {k.dtype} and {v.dtype}")
@@ -803,6 +812,7 @@ def cache4_read(cache: Cache4, slots: torch.Tensor, dtype="f16", stream=None) ->
     _here(cache.device, slots)
     _ints(slots, "slots")
     T = slots.numel()
+    _i32(T)
     dt = _FLOAT_NAME[dtype]
     k, v = cache.data.new_empty((2, T, cache.heads, cache.head_dim), dtype=dt).unbind(0)
     ld = cache.heads * cache.head_dim
@@ -851,6 +861,7 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
     table_ld = _table(block_table, B)
     if max_q is None:
         max_q = 1 if cu_q is None else max(T, 1)
+    _i32(T, Hq, B, block_table.shape[1], max_q, max_ctx, window)
     p = AttentionParams(T, Hq, B, block_table.shape[1], q_ld, _heads(out, "out", (T, Hq, D)), table_ld, max_q, max_ctx,
                         1 if causal else 0, window, D ** -0.5 if scale is None else scale)
     need = lib().qnn_attention4_workspace_size(cache.desc, p)
@@ -877,6 +888,7 @@ def attention4_workspace_size(cache: Cache4, tokens: int, q_heads: int, requests
     """Bytes of workspace of attention4 calls of these sizes (0: none)."""
     if max_q is None:
         max_q = max(tokens, 1)
+    _i32(tokens, q_heads, requests, table_width, max_q, max_ctx, window)
     ld = q_heads * cache.head_dim
     p = AttentionParams(tokens, q_heads, requests, table_width, ld, ld, table_width, max_q, max_ctx, int(bool(causal)),
                         window, 1.0)
@@ -903,6 +915,7 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.
     _ints(free_count, "free_count", 1)
     ld = _table(block_table, B)
     L = lib()
+    _i32(B, page_size, block_table.shape[1], free_pages.numel(), token_capacity)
     need = L.qnn_pages_workspace_size(B)
     if token_capacity < 0:
         raise ValueError("token_capacity must be >= 0")
