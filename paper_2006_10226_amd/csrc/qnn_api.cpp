@@ -2236,9 +2236,10 @@ qnn_status qnn_activation_table(qnn_activation kind, qnn_dtype x_dtype, qnn_qpar
         const double x = (double)x_q.scale[0] * (double)(q - x_q.zero_point[0]);
         double f = 0.0;
         switch (kind) {
-        case QNN_ACT_GELU: f = 0.5 * x * (1.0 + std::erf(x / std::sqrt(2.0))); break;
+        // (1 + erf and 1 + tanh, in forms that keep their digits next to 0)
+        case QNN_ACT_GELU: f = 0.5 * x * std::erfc(-x / std::sqrt(2.0)); break;
         case QNN_ACT_GELU_TANH:
-            f = 0.5 * x * (1.0 + std::tanh(std::sqrt(2.0 / 3.14159265358979323846) * (x + 0.044715 * x * x * x)));
+            f = x / (1.0 + std::exp(-2.0 * std::sqrt(2.0 / 3.14159265358979323846) * (x + 0.044715 * x * x * x)));
             break;
         case QNN_ACT_SILU: f = x / (1.0 + std::exp(-x)); break;
         case QNN_ACT_SIGMOID: f = 1.0 / (1.0 + std::exp(-x)); break;
