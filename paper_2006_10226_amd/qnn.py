@@ -790,6 +790,8 @@ def cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, slots: torch.
     see qnn_cache4_append.  k and v may be slices of a wider tensor of rows."""
     T = k.shape[0]
     _i32(T)
+    if stream is not None and stream.device_index != cache.device:
+        raise ValueError(f"the stream is one of cuda:{stream.device_index}, the cache is on cuda:{cache.device}")
     _here(cache.device, k, v, slots)
     if k.dtype not in _FLOAT_DT or v.dtype != k.dtype:
         raise TypeError(f"k and v must both be f16, bf16, u8 or i8, not {k.dtype} and {v.dtype}")
