@@ -351,8 +351,9 @@ qnn_status qnn_cache4_read(void *stream, qnn_cache4 cache, const int32_t *slots,
  *      Queries past max_q are not computed; max_ctx affects the speed only.
  *   o: device [tokens][q_heads][head_dim], row stride o_ld, FLOAT16, BFLOAT16,
  *      or UINT8 / INT8 (o_q per tensor): round(o / s) + zp, ties to even,
- *      clamped to the dtype (NaN, as from a query that is not finite: zp). Rows of no request (cu_q[requests] on) are left
- *      as they were. Must not overlap q.
+ *      clamped to the dtype (NaN, as from a query that is not finite: zp).
+ *      Rows of no request (cu_q[requests] on) are left as they were. Must not
+ *      overlap q.
  *   workspace: device, 16-byte aligned, of at least
  *      qnn_attention4_workspace_size() bytes (NULL if that is 0), read and
  *      written by this call alone until it is done; contents do not matter.
@@ -360,7 +361,8 @@ qnn_status qnn_cache4_read(void *stream, qnn_cache4 cache, const int32_t *slots,
  * Scores, the softmax and sums are f32; q enters the matrix cores as f16
  * scaled by a power of two (exact for 8-bit values and for f16 and bf16 ones down
  * to 2^-28 of the row's largest; scale * q counts up to 2^121), each weight
- * p_t s_t as one f16, as two where the output has 8 bits. table_width *
+ * p_t s_t as one f16 (off by 2^-11, or 2^-32 of the row's largest), as two where
+ * the output has 8 bits; V's scales count with up to 2^-19 too much. table_width *
  * page_size at most 2^30. The grid has a workgroup for 32 rows (of max_q *
  * q_heads / heads) of every request and cache head, and takes fewer than 2^24 of
  * them (QNN_ERR_UNSUPPORTED else: fewer requests a call, or max_q nearer to their

@@ -34,10 +34,12 @@
 // What bounds it: single tokens read each code once, (DP + 8) bytes for a token's K
 // and V of a head; a step of 32 tokens is about 250 vector instructions for one row
 // block, just under the memory's rate (four requests of 131072 tokens, 8 heads of
-// 128: 105 us, 5.4 TB/s). Prompts hold two row blocks a wave, which share the
-// unpacking (112 of 340 instructions), and are bound by vector instructions: 77% of
-// cycles issue one (2048 queries on 4096 tokens, 32 heads of 128, causal: 177 us,
-// 580 TFLOP/s, matrix cores 25% busy).
+// 128: 107 us, 5.3 TB/s). Prompts hold two row blocks a wave, which share the
+// unpacking (112 of 350 instructions), and are bound by vector instructions, which
+// issue in three quarters of the cycles (2048 queries on 4096 tokens, 32 heads of
+// 128, causal: 182 us, 570 TFLOP/s, matrix cores 25% busy, once the clocks have
+// settled after some 200 calls; 200 to 214 before). A short cache is neither: eight
+// workgroups' chain of loads and eight steps (one request of 1000 tokens 11.6 us).
 #include "cache4.h"
 
 #include <algorithm>
@@ -731,9 +733,18 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs a, int blocks, int c
     store_out(a, (int64_t)(first + i) * a.o_ld + (int64_t)head * a.c.dim + lane * 4, v);
 }
 
-// Least tokens of a part: below, the join's launch and latencies cost more than
-// the walk they save (one request of 1000 tokens 14.0 us in 8 parts, 11.6 us in
-// one; 48 of a window of 1024 24.5 and 21.7 us).
+// Least tokens of a part: below, the join's launch and latencies may cost more than
+// the walk they save, above, more is walked in one part than a join takes. In us,
+// single tokens, by least tokens:              192   384   768   1536
+//   1 request of 1000, 8 x 4 heads of 128     10.4  12.0  11.6  11.6
+//   1 of 1600                                 10.8  11.8  13.8  15.0
+//   1 of 8000                                 11.4  12.4  14.8  18.2
+//   1 of 16000                                14.8  13.0  15.5  19.7
+//   8 of 1600                                 12.7  12.2  14.5  15.6
+//   8 of 4000                                 19.0  16.3  17.4  22.8
+//   48 of 1600, 12 x 1 heads of 64            25.2  25.2  23.7  21.5
+//   48 of 4000                                39.0  38.8  38.7  39.5
+// 768 is never the slowest; few requests would take 192 to 384.
 constexpr int kLeastPart = 768;
 
 struct Shape {

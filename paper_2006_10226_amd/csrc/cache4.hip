@@ -2,9 +2,11 @@
 // neighbouring lanes per vector (a token's K or V of one head), eight channels
 // a lane. The range of a vector comes from shuffles inside its group, so each
 // input is read once and each code written once. 16384 tokens of 8 heads of 128 in
-// f16, 85 MB moved: read back 18.8 us, a copy's rate (4.5 TB/s); written 22 us (3.9
-// TB/s), half of it issuing vector instructions (25 a value: conversion, range,
-// quotient, rounding, addresses), the rest the latency of load and store.
+// f16, 85 MB moved: read back 18.7 us, a copy's rate (4.6 TB/s); written 22.6 us (3.8
+// TB/s; with every eighth token skipped 21.8), bound by vector instructions (25 a
+// value: conversion, range, quotient, rounding, addresses): its 13.1 million wave
+// instructions are 21.3 us of issue at 2.4 GHz. 8-bit rows have half the bytes to
+// read and as many instructions, 24.5 us.
 #include "cache4.h"
 
 #include <algorithm>

@@ -836,11 +836,11 @@ def attention4(q: torch.Tensor, cache: Cache4, block_table: torch.Tensor, ctx: t
     ctx[b] tokens; block_table is int32 [requests][pages].  max_q is at least any
     request's queries, the rest of which stays uncomputed (None: that isn't known,
     all of q, for which the grid is that much larger), max_ctx (0: unknown) about
-    the longest ctx.  scale
-    defaults to head_dim ** -0.5.  The output has y_dtype ("f16", "bf16", "u8",
-    "i8"; q's by default), 8-bit ones with y_scale and y_zp.  `workspace` is a
-    uint8 tensor of attention4_workspace_size() bytes, allocated here if not
-    given; two calls that may overlap need one each."""
+    the longest ctx.  scale defaults to head_dim ** -0.5.  Rows of q behind the last
+    request's stay as they are in the output (in a new one: anything).  The output
+    has y_dtype ("f16", "bf16", "u8", "i8"; q's by default), 8-bit ones with y_scale
+    and y_zp.  `workspace` is a uint8 tensor of attention4_workspace_size() bytes,
+    allocated here if not given; two calls that may overlap need one each."""
     if stream is not None:   # what is allocated here belongs to the stream that uses it
         with torch.cuda.stream(stream):
             return attention4(q, cache, block_table, ctx, cu_q, max_q, max_ctx, scale, causal, window, q_scale, q_zp,
