@@ -362,8 +362,9 @@ qnn_status qnn_cache4_read(void *stream, qnn_cache4 cache, const int32_t *slots,
  * scaled by a power of two (exact for 8-bit values and for f16 and bf16 ones down
  * to 2^-28 of the row's largest; scale * q counts up to 2^121), each weight
  * p_t s_t as one f16 (off by 2^-11, or 2^-32 of the row's largest), as two where
- * the output has 8 bits; V's scales count with up to 2^-19 too much. table_width *
- * page_size at most 2^30. The grid has a workgroup for 32 rows (of max_q *
+ * the output has 8 bits; V's scales count with up to 2^-19 too much. Scales of V
+ * below 2^-104 lose digits, scores of K's scales above 2^119 may overflow.
+ * table_width * page_size at most 2^30. The grid has a workgroup for 32 rows (of max_q *
  * q_heads / heads) of every request and cache head, and takes fewer than 2^24 of
  * them (QNN_ERR_UNSUPPORTED else: fewer requests a call, or max_q nearer to their
  * queries). Enqueued on `stream`, no synchronization.
